@@ -321,6 +321,83 @@ int sjd_gemm_plan(int32_t M, int32_t N, int32_t K, int32_t resid, int32_t *kerne
 int sjd_gemm_bench(int32_t M, int32_t N, int32_t K, int32_t tn, int32_t wk, int32_t u, int32_t iters,
                    float *us_per_launch);
 
+/* ---- microscaled operators ----------------------------------------------------------------------
+ * The operators of a decoder layer whose weights have 4 bits, whose activations have 8 (or 4) and whose
+ * cache has 8.  A 7B layer's weights are 0.27 of their bf16 bytes, a cached token a quarter of what bf16
+ * models store.  Rounded like this a layer is an approximation (E2M1 keeps one mantissa bit): these calls
+ * stand beside sjd_gemm_test and sjd_dist for programs that build such a layer; sjd_step does not use them.
+ *
+ * Numbers.  E4M3: sign, 4 exponent bits (bias 7), 3 mantissa bits, largest 448, 0x7F is NaN, no infinity.
+ * E2M1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, code bit 3 the sign.  Every 32 values along a row
+ * (the cache: the 32 positions of a block x head_dim, keys and values apart) share the scale
+ * 2^(byte - 127), the smallest power of two (byte >= 0) with which the largest finite magnitude does not
+ * exceed 448 (E4M3) or 6 (E2M1) times it: nothing saturates, and rounding to the format (nearest, ties to
+ * even) is the only loss.  The scale byte of a block of zeros is 0.  An infinity or NaN becomes the code
+ * 0x7F (E4M3) and does not count for the scale; E2M1 has no such code: a block that holds one gets the
+ * scale byte 255, which is NaN, and codes 0.
+ * A row of K values is held as Kp = K rounded up to a multiple of 128: codes [rows][Kp] bytes (E4M3) or
+ * [rows][Kp / 2] (E2M1, the first of two values in the low half), scales [rows][Kp / 32]; what lies behind
+ * K is zero.
+ *
+ * dtype: 0 = fp32, 1 = bf16.  ld*: elements from one row to the next (at least the row's length; rows of
+ * a wider matrix may be given).  codes, scales, packed weights, caches and workspaces: 16-byte aligned.
+ * These calls allocate nothing and do not synchronise, so they can be captured into a graph.  A
+ * workspace holds nothing between calls; calls (and captured graphs) that may run at the same time need
+ * one each.                                                                                        */
+#define SJD_MX8 8                  /* E4M3 */
+#define SJD_MX4 4                  /* E2M1 */
+#define SJD_MX_MAX_K (1 << 20)     /* longest row */
+
+/* x dev [rows x K] -> codes, scales in `format`.  up != NULL (dev, like x): of SiLU(x) * up instead.   */
+int sjd_mx_quantize(int32_t format, int32_t dtype, const void *x, const void *up, int64_t ld, int32_t rows, int32_t K,
+                    uint8_t *codes, uint8_t *scales, void *stream);
+
+/* h = resid + x, kept in resid (dev fp32 [rows x d], in and out); h / sqrt(mean(h^2) + eps) * gain -> codes,
+ * scales in `format`.  gain dev fp32 [d].  x NULL: h = resid (dtype and ldx are ignored); resid NULL: h = x, and nothing is kept.
+ * Not both.  Sums in fp32.                                                                          */
+int sjd_mx_rmsnorm(int32_t format, int32_t dtype, const void *x, int64_t ldx, float *resid, int64_t ldr, const float *gain,
+                   float eps, int32_t rows, int32_t d, uint8_t *codes, uint8_t *scales, void *stream);
+
+/* Weights W dev [N x K] -> E2M1, in the order in which the product streams them.  Tile t (16 features) and group
+ * g (512 values) are one record of 4352 bytes at (t * ceil(K / 512) + g) * 4352.  Byte 1024 s + 16 (16 q + f) + j holds
+ * W[16 t + f][512 g + 128 s + 32 q + 2 j] (low half) and the next value; byte 4096 + 4 (16 q + f) + s their
+ * scale.  What lies behind N or K is zero.  sjd_mx_weights_bytes: the size.                            */
+int sjd_mx_weights_bytes(int32_t N, int32_t K, size_t *bytes);
+int sjd_mx_weights(int32_t dtype, const void *W, int64_t ld, int32_t N, int32_t K, uint8_t *packed, void *stream);
+
+/* C[M x N] (dev, dtype, row length ldc) = A W^T: A codes and scales in `format` as above (K values a row), W packed.  fp32 results:
+ * products of codes are exact, sums are fp32.  bf16 results: of eight neighbouring products those below 2^-13 of the largest are cut
+ * (5e-6 of a result), sums are fp32 and rounded once.  workspace: sjd_mx_product_workspace bytes (may be 0).   */
+int sjd_mx_product_workspace(int32_t M, int32_t N, int32_t K, size_t *bytes);
+int sjd_mx_product(int32_t format, const uint8_t *codes, const uint8_t *scales, const uint8_t *packed, int32_t M, int32_t N,
+                   int32_t K, int32_t dtype, void *C, int64_t ldc, void *workspace, size_t workspace_bytes, void *stream);
+
+/* A cache in 8 bits of n_seqs sequences, `cap` positions each: cache dev [n_seqs][n_kv_heads][ceil(cap / 32)][64 * head_dim],
+ * scales dev [n_seqs][n_kv_heads][ceil(cap / 32)][2] (keys, values).  head_dim: a multiple of 32, at most 256.  A block's record
+ * holds its keys, then its values, as the lanes of the attention read them:
+ *   K[p][d] at 1024 (o / 2) + 16 l + 8 (o % 2) + d % 8, o = (p / 16)(head_dim / 32) + d / 32, l = 16 (d % 32 / 8) + p % 16
+ *   V[p][d] at 32 head_dim + 1024 (o / 2) + 16 l + 8 (o % 2) + 4 (p / 16) + p % 4, o = d / 16, l = 16 (p % 16 / 4) + d % 16
+ * len dev [n_seqs]: cached positions per sequence before the window; the window's L tokens are positions len .. len + L - 1.
+ * A sequence with len < 0 or len + L > cap sits out: neither its cache nor its rows of `out` are touched.
+ *
+ * sjd_kv8_append: k, v dev [n_seqs * L][n_kv_heads * head_dim] (rows of length ld) into the cache.  The scale of a block that holds
+ * positions already is made anew from those and the new ones; their codes move to it (exact but for codes that become
+ * subnormal).  Positions of a touched block behind the window are zero afterwards; other blocks are not touched.  A window may be
+ * appended again at the same or a smaller len (after a rejection).  len itself is the caller's to advance.        */
+int sjd_kv8_append(int32_t dtype, const void *k, const void *v, int64_t ld, const int32_t *len, int32_t n_seqs, int32_t L,
+                   int32_t n_kv_heads, int32_t head_dim, int32_t cap, uint8_t *cache, uint8_t *scales, void *stream);
+
+/* Attention of the window's queries q dev [n_seqs * L][n_heads * head_dim] (rows of length ldq) over the cache, the appended window
+ * included: softmax(q k / sqrt(head_dim)) v.  The query at position p sees the positions j <= p with, if window > 0, also
+ * j > p - window or j < sinks.  Query head h reads cache head h / (n_heads / n_kv_heads).  out dev, like q, rows of length ldo,
+ * of the same dtype (which also says how finely probabilities are held: 22 bits for fp32, 11 for bf16).  workspace:
+ * sjd_kv8_attention_workspace bytes.  What masked positions hold, NaN included, does not reach `out`.               */
+int sjd_kv8_attention_workspace(int32_t n_seqs, int32_t L, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t cap,
+                                size_t *bytes);
+int sjd_kv8_attention(int32_t dtype, const void *q, int64_t ldq, const uint8_t *cache, const uint8_t *scales, const int32_t *len,
+                      int32_t n_seqs, int32_t L, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t cap, int32_t window,
+                      int32_t sinks, void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
+
 const char *sjd_strerror(int code);
 
 #ifdef __cplusplus

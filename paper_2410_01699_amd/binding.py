@@ -19,13 +19,17 @@ SJD_STATIC_VERIFY_FLOATS = 17 * 16384
 SJD_MAX_WINDOW = 64
 SJD_MAX_ROWS = 128          # rows one forward computes (window x contexts x images)
 SJD_MAX_SAMP_VOCAB = 32768
+SJD_MX8, SJD_MX4 = 8, 4     # microscaled formats: E4M3, E2M1
+SJD_MX_MAX_K = 1 << 20
 
 EXPORTS = ["sjd_init_model", "sjd_free_model", "sjd_kv_create", "sjd_kv_free", "sjd_kv_reset", "sjd_kv_len",
            "sjd_kv_set_len", "sjd_prefill", "sjd_first_window", "sjd_step", "sjd_generate", "sjd_forward_logits",
            "sjd_verify", "sjd_verify_probs", "sjd_dist", "sjd_gemm_test", "sjd_strerror", "sjd_decode_begin",
            "sjd_decode_steps", "sjd_decode_status", "sjd_decode_result", "sjd_kv_use_graph", "sjd_profile_steps", "sjd_gemm_bench",
            "sjd_prefill_uncond", "sjd_generate_cfg", "sjd_decode_steps_batch", "sjd_forward_logits_batch",
-           "sjd_generate_batch", "sjd_profile_steps_batch", "sjd_verify_static", "sjd_gemm_plan"]
+           "sjd_generate_batch", "sjd_profile_steps_batch", "sjd_verify_static", "sjd_gemm_plan",
+           "sjd_mx_quantize", "sjd_mx_rmsnorm", "sjd_mx_weights_bytes", "sjd_mx_weights", "sjd_mx_product_workspace", "sjd_mx_product",
+           "sjd_kv8_append", "sjd_kv8_attention_workspace", "sjd_kv8_attention"]
 
 PROF_KINDS = ("gemm", "attention", "elementwise", "verify")
 
@@ -65,7 +69,7 @@ if not os.path.exists(LIB_PATH):
                       "(there is no CPU fallback)")
 _lib = C.CDLL(LIB_PATH)
 
-_vp, _i32, _u64, _sz = C.c_void_p, C.c_int32, C.c_uint64, C.c_size_t
+_vp, _i32, _i64, _u64, _sz = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64, C.c_size_t
 _P = C.POINTER
 _SIG = {
     "sjd_init_model": (C.c_int, [_P(sjd_config), _vp, _sz, _P(_vp)]),
@@ -106,6 +110,16 @@ _SIG = {
     "sjd_decode_result": (C.c_int, [_vp, _vp, _P(sjd_stats)]),
     "sjd_kv_use_graph": (C.c_int, [_vp, _i32]),
     "sjd_profile_steps": (C.c_int, [_vp, _vp, _i32, _P(sjd_profile), _vp]),
+    "sjd_mx_quantize": (C.c_int, [_i32, _i32, _vp, _vp, _i64, _i32, _i32, _vp, _vp, _vp]),
+    "sjd_mx_rmsnorm": (C.c_int, [_i32, _i32, _vp, _i64, _vp, _i64, _vp, C.c_float, _i32, _i32, _vp, _vp, _vp]),
+    "sjd_mx_weights_bytes": (C.c_int, [_i32, _i32, _P(_sz)]),
+    "sjd_mx_weights": (C.c_int, [_i32, _vp, _i64, _i32, _i32, _vp, _vp]),
+    "sjd_mx_product_workspace": (C.c_int, [_i32, _i32, _i32, _P(_sz)]),
+    "sjd_mx_product": (C.c_int, [_i32, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _sz, _vp]),
+    "sjd_kv8_append": (C.c_int, [_i32, _vp, _vp, _i64, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp]),
+    "sjd_kv8_attention_workspace": (C.c_int, [_i32, _i32, _i32, _i32, _i32, _i32, _P(_sz)]),
+    "sjd_kv8_attention": (C.c_int, [_i32, _vp, _i64, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _sz,
+                                    _vp]),
     "sjd_gemm_bench": (C.c_int, [_i32, _i32, _i32, _i32, _i32, _i32, _i32, _P(C.c_float)]),
 }
 for _name, (_res, _args) in _SIG.items():
@@ -342,3 +356,128 @@ def sjd_gemm_bench(M, N, K, tn, wk, u, iters=50) -> float:
     us = C.c_float(0)
     _check(_lib.sjd_gemm_bench(M, N, K, tn, wk, u, iters, C.byref(us)))
     return us.value
+
+
+# ---- microscaled operators ------------------------------------------------------------------------
+# Matrices may be rows of wider ones (last dimension contiguous); everything else is contiguous.  A tensor that is on another
+# device than the current one, or too small for what the call reads or writes, is refused.
+def _need(ok, what):
+    if not ok:
+        raise SjdError(SJD_EINVAL, what)
+
+
+def _here(name, t, dtypes):
+    import torch
+    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{name} is not on the current device")
+    _need(str(t.dtype)[6:] in dtypes, f"{name} is {t.dtype}, not {' or '.join(dtypes)}")
+    return t
+
+
+def _rows(name, t, rows, cols, dtypes=("float32", "bfloat16")):
+    """(address, dtype code, elements from row to row) of a [rows, cols] matrix; None -> NULL"""
+    if t is None:
+        return None, 0, 0
+    _here(name, t, dtypes)
+    _need(tuple(t.shape) == (rows, cols), f"{name} is {tuple(t.shape)}, not {(rows, cols)}")
+    _need((cols == 1 or t.stride(1) == 1) and (rows == 1 or t.stride(0) >= cols), f"{name}: rows are not contiguous, or overlap")
+    return C.c_void_p(t.data_ptr()), int(t.dtype.itemsize == 2), cols if rows == 1 else t.stride(0)
+
+
+def _flat(name, t, count, dtype="uint8", exact=True):
+    """address of a contiguous tensor of `count` elements (or at least as many)"""
+    _here(name, t, (dtype,))
+    _need(t.is_contiguous() and (t.numel() == count if exact else t.numel() >= count), f"{name}: {count} contiguous elements are needed, got {tuple(t.shape)}")
+    return C.c_void_p(t.data_ptr())
+
+
+def _coded(format, rows, K, codes, scales):
+    """addresses of a matrix's codes and scales"""
+    _need(format in (SJD_MX8, SJD_MX4), "format is SJD_MX8 or SJD_MX4")
+    Kp = -(-K // 128) * 128
+    return _flat("codes", codes, rows * Kp * format // 8), _flat("scales", scales, rows * Kp // 32)
+
+
+def _workspace(workspace, need):
+    return (None, 0) if not need else (_flat("workspace", workspace, need, exact=False), workspace.numel())
+
+
+def sjd_mx_quantize(format, x, codes, scales, up=None, stream=None):
+    """x: device [rows, K] (up: the same, then of SiLU(x) * up) -> codes, scales"""
+    _need(x.dim() == 2, "x is a matrix")
+    rows, K = x.shape
+    px, dt, ld = _rows("x", x, rows, K)
+    pu, du, lu = _rows("up", up, rows, K)
+    _need(up is None or (du == dt and lu == ld), "x and up have the same type and stride")
+    _check(_lib.sjd_mx_quantize(format, dt, px, pu, ld, rows, K, *_coded(format, rows, K, codes, scales), _stream(stream)))
+
+
+def sjd_mx_rmsnorm(format, x, resid, gain, eps, codes, scales, stream=None):
+    """x [rows, d] (or None) added to resid fp32 [rows, d] (in place; or None), normalised -> codes, scales"""
+    of = x if x is not None else resid
+    _need(of is not None and of.dim() == 2, "x or resid is a matrix")
+    rows, d = of.shape
+    px, dt, ldx = _rows("x", x, rows, d)
+    pr, _, ldr = _rows("resid", resid, rows, d, ("float32",))
+    _check(_lib.sjd_mx_rmsnorm(format, dt, px, ldx, pr, ldr, _flat("gain", gain, d, "float32"), eps, rows, d,
+                               *_coded(format, rows, d, codes, scales), _stream(stream)))
+
+
+def sjd_mx_weights_bytes(N, K) -> int:
+    n = _sz(0)
+    _check(_lib.sjd_mx_weights_bytes(N, K, C.byref(n)))
+    return n.value
+
+
+def sjd_mx_weights(W, packed, stream=None):
+    """W: device [N, K] -> packed: device uint8, sjd_mx_weights_bytes(N, K) of them"""
+    _need(W.dim() == 2, "W is a matrix")
+    N, K = W.shape
+    pw, dt, ld = _rows("W", W, N, K)
+    _check(_lib.sjd_mx_weights(dt, pw, ld, N, K, _flat("packed", packed, sjd_mx_weights_bytes(N, K)), _stream(stream)))
+
+
+def sjd_mx_product_workspace(M, N, K) -> int:
+    n = _sz(0)
+    _check(_lib.sjd_mx_product_workspace(M, N, K, C.byref(n)))
+    return n.value
+
+
+def sjd_mx_product(format, codes, scales, packed, K, out, workspace, stream=None):
+    """out [M, N] = the rows behind codes and scales (K values each) times the packed weights"""
+    _need(out.dim() == 2, "out is a matrix")
+    M, N = out.shape
+    po, dt, ld = _rows("out", out, M, N)
+    _check(_lib.sjd_mx_product(format, *_coded(format, M, K, codes, scales), _flat("packed", packed, sjd_mx_weights_bytes(N, K)), M, N, K,
+                               dt, po, ld, *_workspace(workspace, sjd_mx_product_workspace(M, N, K)), _stream(stream)))
+
+
+def _kv8(cache, scales, n_seqs, n_kv, hd, cap):
+    blocks = n_seqs * n_kv * -(-cap // 32)
+    return _flat("cache", cache, blocks * 64 * hd), _flat("scales", scales, blocks * 2)
+
+
+def sjd_kv8_append(k, v, length, L, n_kv, hd, cap, cache, scales, stream=None):
+    """k, v: device [n_seqs * L, n_kv * hd]; length: device int32 [n_seqs]"""
+    n_seqs = length.numel()
+    pk, dt, ld = _rows("k", k, n_seqs * L, n_kv * hd)
+    pv, dv, lv = _rows("v", v, n_seqs * L, n_kv * hd)
+    _need(dt == dv and ld == lv, "k and v have the same type and stride")
+    _check(_lib.sjd_kv8_append(dt, pk, pv, ld, _flat("length", length, n_seqs, "int32"), n_seqs, L, n_kv, hd, cap,
+                               *_kv8(cache, scales, n_seqs, n_kv, hd, cap), _stream(stream)))
+
+
+def sjd_kv8_attention_workspace(n_seqs, L, n_heads, n_kv, hd, cap) -> int:
+    n = _sz(0)
+    _check(_lib.sjd_kv8_attention_workspace(n_seqs, L, n_heads, n_kv, hd, cap, C.byref(n)))
+    return n.value
+
+
+def sjd_kv8_attention(q, cache, scales, length, L, n_heads, n_kv, hd, cap, window, sinks, out, workspace, stream=None):
+    """q, out: device [n_seqs * L, n_heads * hd] of one type; window 0: everything up to the query's position"""
+    n_seqs = length.numel()
+    pq, dt, ldq = _rows("q", q, n_seqs * L, n_heads * hd)
+    po, do, ldo = _rows("out", out, n_seqs * L, n_heads * hd)
+    _need(dt == do, "q and out have the same type")
+    need = sjd_kv8_attention_workspace(n_seqs, L, n_heads, n_kv, hd, cap)
+    _check(_lib.sjd_kv8_attention(dt, pq, ldq, *_kv8(cache, scales, n_seqs, n_kv, hd, cap), _flat("length", length, n_seqs, "int32"), n_seqs, L,
+                                  n_heads, n_kv, hd, cap, window, sinks, po, ldo, *_workspace(workspace, need), _stream(stream)))

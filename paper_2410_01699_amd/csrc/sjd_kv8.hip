@@ -1,0 +1,505 @@
+// A cache of keys and values in 8 bits (E4M3) with a power-of-two scale per block of 32 positions and head: appending a window, and the
+// window's attention over it.
+//
+// A block's record holds keys and values as v_mfma_f32_16x16x32_f16 takes them, two operands (8 codes each) to the 16 bytes of a lane,
+// so a wave reads a record as contiguous KiB loads.  Codes become fp16 exactly; scales stay outside the products.
+#include "sjd_mx.h"
+
+#include <algorithm>
+
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+
+#define KV8_MAX_SEQS 32767
+#define KV8_MAX_HEADS 65535
+
+static bool kv8_sizes(int n_seqs, int L, int n_kv, int hd, int cap)
+{
+    if (n_seqs < 1 || n_seqs > KV8_MAX_SEQS || L < 1 || n_kv < 1 || n_kv > KV8_MAX_HEADS || cap < 1 || cap > INT32_MAX - 64 || L > cap) return false;
+    return hd == 32 || hd == 64 || hd == 96 || hd == 128 || hd == 256;
+}
+
+// ---- append ---------------------------------------------------------------------------------
+// A workgroup makes the keys (or the values) of one block: new rows and the codes that the block holds already meet in LDS as fp32,
+// their largest magnitude gives the scale, and a thread then makes 16 bytes of the record.
+template <typename T>
+__global__ __launch_bounds__(512) void kv8_append_kernel(const T *__restrict__ k, const T *__restrict__ v, int64_t ld,
+                                                         const int32_t *__restrict__ len, int L, int hd, int cap, int nblk, int vec,
+                                                         uint8_t *__restrict__ cache, uint8_t *__restrict__ scales)
+{
+    extern __shared__ float tile[];                         // [32][hd + 4]
+    __shared__ uint32_t top[8];
+    const int which = blockIdx.z & 1, b = blockIdx.z >> 1, head = blockIdx.y, tid = threadIdx.x;
+    const int n = len[b];
+    if (n < 0 || n > cap - L) return;
+    const int blk = (n >> 5) + (int)blockIdx.x, p0 = blk * 32;
+    if (p0 >= n + L) return;
+    const int pitch = hd + 4, held = min(max(n - p0, 0), 32);
+    const size_t at = ((size_t)b * gridDim.y + head) * nblk + blk;
+    uint8_t *rec = cache + at * 64 * hd + (size_t)which * 32 * hd;
+    const T *src = (which ? v : k) + (size_t)head * hd;
+    // code group of this thread: two operands of eight codes (2 hd threads)
+    const int pair = tid >> 6, lane = tid & 63, ks = hd >> 5;
+    auto place = [&](int half, int e, int &p, int &d) {
+        const int o = pair * 2 + half;
+        if (which) { d = o * 16 + (lane & 15); p = (e >> 2) * 16 + (lane >> 4) * 4 + (e & 3); }
+        else { p = o / ks * 16 + (lane & 15); d = o % ks * 32 + (lane >> 4) * 8 + e; }
+    };
+    uint32_t amax = 0;
+    for (int u = tid; u < hd * 4; u += blockDim.x) {        // eight values of a new row, or zeros behind the window
+        const int p = u / (hd / 8), c = u % (hd / 8) * 8;
+        if (p < held) continue;
+        float x[8];
+        if (p0 + p < n + L) {
+            mx_load8<T>(src + ((size_t)b * L + (p0 + p - n)) * ld, c, hd, vec, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) amax = max(amax, mx_finite_bits(x[i]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.f;
+        }
+        float4 *dst = reinterpret_cast<float4 *>(tile + p * pitch + c);
+        dst[0] = make_float4(x[0], x[1], x[2], x[3]); dst[1] = make_float4(x[4], x[5], x[6], x[7]);
+    }
+    if (held) {
+        const uint4 old = reinterpret_cast<const uint4 *>(rec)[tid];
+        const float s = mx_pow2(scales[at * 2 + which]);
+        const uint32_t w[4] = {old.x, old.y, old.z, old.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], true);
+            const float x[4] = {lo.x * s, lo.y * s, hi.x * s, hi.y * s};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                int p, d;
+                place(i >> 1, (i & 1) * 4 + j, p, d);
+                if (p < held) { tile[p * pitch + d] = x[j]; amax = max(amax, mx_finite_bits(x[j])); }
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o));
+    if (lane == 0) top[tid >> 6] = amax;
+    __syncthreads();
+    for (int w = 0; w < (int)blockDim.x / 64; ++w) amax = max(amax, top[w]);
+    const int byte = mx_scale_byte<SJD_MX8>(amax);
+    const float inv = mx_pow2(254 - byte);
+    uint32_t out[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            int p, d;
+            place(i >> 1, (i & 1) * 4 + j, p, d);
+            x[j] = tile[p * pitch + d];
+        }
+        out[i] = mx_e4m3x4(x[0], x[1], x[2], x[3], inv);
+    }
+    reinterpret_cast<uint4 *>(rec)[tid] = make_uint4(out[0], out[1], out[2], out[3]);
+    if (tid == 0) scales[at * 2 + which] = (uint8_t)byte;
+}
+
+extern "C" int sjd_kv8_append(int32_t dtype, const void *k, const void *v, int64_t ld, const int32_t *len, int32_t n_seqs, int32_t L,
+                              int32_t n_kv_heads, int32_t head_dim, int32_t cap, uint8_t *cache, uint8_t *scales, void *stream)
+{
+    if (!k || !v || !len || !cache || !scales || (dtype != 0 && dtype != 1)) return SJD_EINVAL;
+    if (!kv8_sizes(n_seqs, L, n_kv_heads, head_dim, cap) || ld < (int64_t)n_kv_heads * head_dim || !mx_aligned(cache) || !mx_aligned(scales)) return SJD_EINVAL;
+    const dim3 grid((L + 31) / 32 + 1, n_kv_heads, n_seqs * 2), block(2 * head_dim);
+    const int vec = mx_vec(k, ld, dtype) && mx_vec(v, ld, dtype);
+    const size_t lds = 32 * (head_dim + 4) * sizeof(float);
+    hipStream_t s = (hipStream_t)stream;
+    const int nblk = (cap + 31) / 32;
+    if (dtype == 0) SJD_LAUNCH((kv8_append_kernel<float>), grid, block, lds, s, (const float *)k, (const float *)v, ld, len, L, head_dim, cap, nblk, vec, cache, scales);
+    else SJD_LAUNCH((kv8_append_kernel<bf16_t>), grid, block, lds, s, (const bf16_t *)k, (const bf16_t *)v, ld, len, L, head_dim, cap, nblk, vec, cache, scales);
+    HIP_TRY(hipGetLastError());
+    return SJD_OK;
+}
+
+// ---- attention ------------------------------------------------------------------------------
+// The queries of one sequence that read one cache head, L * (heads per cache head) rows with a query's heads next to each other, are cut
+// into groups of 16 or 32 rows.  A (sequence, group) pair walks the blocks that any of its queries sees, the sinks' first.  Where the
+// pairs are too few for the chip their walks are cut into splits, all of about the same number of blocks: lengths live on the device,
+// so the kernels work the cut out themselves, every workgroup the same.
+struct Kv8Plan {
+    const int32_t *len;
+    int32_t n_seqs, L, group, qgroups, rg;     // heads per cache head; row groups of `rg` rows per sequence
+    int32_t window, sinks, cap, nblk;
+    int32_t slots;                             // splits to aim for per cache head; 0: one per pair, none cut
+};
+struct Kv8Span { int32_t i0, i1, n, first, front, count; };    // queries, cached positions; block v is v < front ? v : first + v - front
+__device__ __forceinline__ Kv8Span kv8_span(const Kv8Plan &pl, int pair)
+{
+    Kv8Span s;
+    const int b = pair / pl.qgroups, r0 = (pair - b * pl.qgroups) * pl.rg;
+    s.n = pl.len[b];
+    s.i0 = r0 / pl.group;
+    s.i1 = min(r0 + pl.rg - 1, pl.L * pl.group - 1) / pl.group;
+    s.first = s.front = s.count = 0;
+    if (s.n < 0 || s.n > pl.cap - pl.L) return s;
+    const int last = s.n + s.i1;
+    if (pl.window) {
+        s.first = max(0, s.n + s.i0 - pl.window + 1) >> 5;
+        s.front = min((min(pl.sinks, last + 1) + 31) >> 5, s.first);
+    }
+    s.count = s.front + (last >> 5) - s.first + 1;
+    return s;
+}
+struct Kv8Part { int32_t pair, split, splits, per, base; };     // a slot's pair, its place among the pair's splits, blocks per split
+// lanes look at 64 pairs at a time; by_pair: the part that starts the given pair, else the part of the given slot
+__device__ __forceinline__ bool kv8_part(const Kv8Plan &pl, int want, bool by_pair, Kv8Part &part)
+{
+    const int pairs = pl.n_seqs * pl.qgroups, lane = threadIdx.x & 63;
+    int64_t total = 0;
+    for (int p0 = 0; p0 < pairs; p0 += 64) {
+        int64_t c = p0 + lane < pairs ? kv8_span(pl, p0 + lane).count : 0;
+#pragma unroll
+        for (int o = 32; o; o >>= 1) c += __shfl_xor(c, o);
+        total += c;
+    }
+    part.per = max(4, (int)((total + pl.slots - 1) / pl.slots));
+    int base = 0;
+    for (int p0 = 0; p0 < pairs; p0 += 64) {
+        const int c = p0 + lane < pairs ? kv8_span(pl, p0 + lane).count : 0;
+        const int mine = (c + part.per - 1) / part.per;
+        int incl = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) { const int up = __shfl_up(incl, o); if (lane >= o) incl += up; }
+        const int start = base + incl - mine;
+        const uint64_t hit = by_pair ? __ballot(p0 + lane == want) : __ballot(want >= start && want < start + mine);
+        if (hit) {
+            const int l = __ffsll((unsigned long long)hit) - 1;
+            part.pair = p0 + l;
+            part.splits = __shfl(mine, l);
+            part.base = __shfl(start, l);
+            part.split = by_pair ? 0 : want - part.base;
+            return true;
+        }
+        base += __shfl(incl, 63);
+    }
+    return false;
+}
+
+__device__ __forceinline__ f16x8 kv8_f16(uint32_t lo, uint32_t hi)        // eight codes
+{
+    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
+    const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
+    return (f16x8){a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+// bytes 0x80 where a code is NaN (0x7F with any sign)
+__device__ __forceinline__ uint32_t kv8_nan(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ float kv8_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ void kv8_put(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
+
+#define KV8_WAVES 4
+#define KV8_LIFT 14      // probabilities times 2^14 in fp16: 22 bits of hi + lo hold from 2^-27 of the largest on
+// record of a split: O[rg][HD] in units of 2^(mo - KV8_LIFT), then m[rg], mo[rg], l[rg]
+__host__ __device__ __forceinline__ size_t kv8_record(int rg, int hd) { return (size_t)rg * (hd + 3); }
+
+__device__ __forceinline__ float kv8_load(const float *p) { return *p; }
+__device__ __forceinline__ float kv8_load(const bf16_t *p) { return bf16_to_f32(*p); }
+__device__ __forceinline__ void kv8_out(float *p, const f32x4 &v, bool vec)
+{
+    if (vec) *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    else { p[0] = v[0]; p[1] = v[1]; p[2] = v[2]; p[3] = v[3]; }
+}
+__device__ __forceinline__ void kv8_out(bf16_t *p, const f32x4 &v, bool vec)
+{
+    if (vec) *reinterpret_cast<uint2 *>(p) = make_uint2(f32_to_bf16(v[0]) | (uint32_t)f32_to_bf16(v[1]) << 16,
+                                                        f32_to_bf16(v[2]) | (uint32_t)f32_to_bf16(v[3]) << 16);
+    else { p[0] = f32_to_bf16(v[0]); p[1] = f32_to_bf16(v[1]); p[2] = f32_to_bf16(v[2]); p[3] = f32_to_bf16(v[3]); }
+}
+
+// Per block of 32 positions, with the scales 2^ek and 2^ev of its keys and values:
+//   S^T[key][row] = K codes . Q (Q scaled per row to 2^13 .. 2^14, hi + lo fp16)        s = S * 2^ek * 2^eq * log2(e) / sqrt(HD)
+//   m = max s, l = sum 2^(s - m);   mo = max (s + ev):  O = sum 2^(s + ev - mo + LIFT) * V codes
+// O has a reference of its own because the blocks' scales differ: with it the largest contribution is always 2^LIFT, whatever the
+// scales are, and fp16 holds what matters beside it.  out = O * 2^(mo - LIFT - m) / l.
+// The two score tiles of a block leave lane (g, c) with row c and the positions 16 h + 4 g + i: the order in which V's operands hold them.
+template <int HD, int MT, typename T>
+__global__ __launch_bounds__(64 * KV8_WAVES) void kv8_attention_kernel(const T *__restrict__ q, int64_t ldq, const uint8_t *__restrict__ cache,
+                                                                       const uint8_t *__restrict__ scales, Kv8Plan pl, T *__restrict__ out,
+                                                                       int64_t ldo, int vec, float *__restrict__ part)
+{
+    constexpr int KS = HD / 32, DT = HD / 16, RG = MT * 16, PL = sizeof(T) == 4 ? 2 : 1, CH = DT < 8 ? DT : 8;
+    __shared__ f16x8 q_lds[MT][KS][PL][64];
+    __shared__ float q_scale[RG];
+    __shared__ float m_all[KV8_WAVES][RG], mo_all[KV8_WAVES][RG], l_all[KV8_WAVES][RG];
+    __shared__ f32x4 o_slot[KV8_WAVES][CH][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
+    const int head = blockIdx.x, heads = gridDim.x;
+    Kv8Part pt = {(int)blockIdx.y, 0, 1, 0, 0};
+    if (pl.slots && !kv8_part(pl, (int)blockIdx.y, false, pt)) return;
+    const Kv8Span sp = kv8_span(pl, pt.pair);
+    if (!sp.count) return;
+    const int per = pl.slots ? pt.per : sp.count;
+    const int v_beg = pt.split * per, v_end = min(sp.count, v_beg + per);
+    const int b = pt.pair / pl.qgroups, r0 = (pt.pair - b * pl.qgroups) * RG, rows = pl.L * pl.group;
+
+    // Q of row tile mt by wave mt: lane (g, c) has values 32 ks + 8 g .. of row c
+    if (wave < MT) {
+        const int r = r0 + wave * 16 + c;
+        float x[KS][8];
+        uint32_t top = 0;
+        const T *src = q + ((size_t)b * pl.L + min(r, rows - 1) / pl.group) * ldq + ((size_t)head * pl.group + min(r, rows - 1) % pl.group) * HD;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            mx_load8<T>(src, ks * 32 + g * 8, HD, vec & 1, x[ks]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, mx_finite_bits(x[ks][e]));
+        }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        const int up = min(max(127 + 13 - (int)(top >> 23), -126), 127);        // 2^up * the largest is in 2^13 .. 2^14
+        const float mul = mx_pow2(127 + up);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            f16x8 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float y = x[ks][e] * mul;
+                hi[e] = (_Float16)y;
+                lo[e] = (_Float16)(y - (float)hi[e]);
+            }
+            q_lds[wave][ks][0][lane] = hi;
+            if (PL == 2) q_lds[wave][ks][PL - 1][lane] = lo;
+        }
+        if (g == 0) q_scale[wave * 16 + c] = mx_pow2(127 - up) * (1.4426950408889634f / sqrtf((float)HD));
+    }
+    __syncthreads();
+
+    f32x4 o[MT][DT];
+    float m[MT], mo[MT], l[MT], qs[MT];
+    int pos[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        m[mt] = mo[mt] = -INFINITY; l[mt] = 0.f;
+        qs[mt] = q_scale[mt * 16 + c];
+        pos[mt] = sp.n + min(r0 + mt * 16 + c, rows - 1) / pl.group;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[mt][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    const size_t at0 = ((size_t)b * heads + head) * pl.nblk;
+    for (int v = v_beg + wave; v < v_end; v += KV8_WAVES) {
+        const int blk = v < sp.front ? v : sp.first + v - sp.front, k0 = blk * 32;
+        const uint4 *rec = reinterpret_cast<const uint4 *>(cache + (at0 + blk) * (64 * HD)) + lane;
+        uint4 ka[KS], va[KS];
+#pragma unroll
+        for (int p = 0; p < KS; ++p) ka[p] = rec[p * 64];
+#pragma unroll
+        for (int p = 0; p < KS; ++p) va[p] = rec[(KS + p) * 64];
+        const int sc = *reinterpret_cast<const uint16_t *>(scales + (at0 + blk) * 2);
+        const float ks2 = mx_pow2(sc & 255), ev = (float)((sc >> 8) - 127);
+        const bool whole = k0 + 31 <= sp.n + sp.i0 && (!pl.window || k0 > sp.n + sp.i1 - pl.window || k0 + 31 < pl.sinks);
+        f32x4 s[MT][2];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) s[mt][0] = s[mt][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int op = 0; op < 2 * KS; ++op) {
+            const int h = op / KS, ks = op % KS;
+            const f16x8 k = (op & 1) ? kv8_f16(ka[op / 2].z, ka[op / 2].w) : kv8_f16(ka[op / 2].x, ka[op / 2].y);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                for (int p = PL - 1; p >= 0; --p) s[mt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q_lds[mt][ks][p][lane], s[mt][h], 0, 0, 0);
+            }
+        }
+        bool nan = false;
+        if (!whole) {                         // NaN among values that a mask hides from some row
+            uint32_t any = 0;
+#pragma unroll
+            for (int p = 0; p < KS; ++p) any |= kv8_nan(va[p].x) | kv8_nan(va[p].y) | kv8_nan(va[p].z) | kv8_nan(va[p].w);
+            nan = __ballot(any != 0) != 0;
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            float x[8], bm = -INFINITY;
+            bool see[8];
+            const float cs = qs[mt] * ks2;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int key = k0 + (e >> 2) * 16 + g * 4 + (e & 3);
+                see[e] = whole || (key <= pos[mt] && (!pl.window || key > pos[mt] - pl.window || key < pl.sinks));
+                x[e] = see[e] ? s[mt][e >> 2][e & 3] * cs : -INFINITY;
+                bm = fmaxf(bm, x[e]);
+            }
+            bm = fmaxf(bm, __shfl_xor(bm, 16));
+            bm = fmaxf(bm, __shfl_xor(bm, 32));
+            const float mn = fmaxf(m[mt], bm), mon = fmaxf(mo[mt], bm + ev);
+            const float so = mn == -INFINITY ? 1.f : kv8_exp2(m[mt] - mn), soo = mon == -INFINITY ? 1.f : kv8_exp2(mo[mt] - mon);
+            const float f = mn == -INFINITY ? 0.f : kv8_exp2(fminf(ev - mon + mn + KV8_LIFT, 120.f));
+            float sum = 0.f;
+            f16x8 ph, plo;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float p = see[e] ? kv8_exp2(x[e] - mn) : 0.f;
+                sum += p;
+                float pf = p * f;
+                asm("" : "+v"(pf));          // (the product in fp32 for both parts: fused into the conversion to fp16 it rounds otherwise now and then)
+                ph[e] = (_Float16)pf;
+                plo[e] = (_Float16)(pf - (float)ph[e]);
+            }
+            l[mt] = l[mt] * so + sum;
+            m[mt] = mn; mo[mt] = mon;
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                uint32_t w0 = (t & 1) ? va[t / 2].z : va[t / 2].x, w1 = (t & 1) ? va[t / 2].w : va[t / 2].y;
+                o[mt][t] *= soo;
+                if (nan) {
+                    // zero times NaN is NaN: NaN codes are taken out, and the rows that see one get it by counting
+                    const uint32_t n0 = kv8_nan(w0) >> 7, n1 = kv8_nan(w1) >> 7;        // 1 in the byte of a NaN
+                    f16x8 ind, vis;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        ind[e] = (_Float16)(float)(((e < 4 ? n0 : n1) >> (8 * (e & 3))) & 1u);
+                        vis[e] = see[e] ? (_Float16)1.f : (_Float16)0.f;
+                    }
+                    f32x4 hits = {0.f, 0.f, 0.f, 0.f};
+                    hits = __builtin_amdgcn_mfma_f32_16x16x32_f16(ind, vis, hits, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) if (hits[i] != 0.f) o[mt][t][i] = NAN;
+                    w0 &= ~(n0 * 0xFFu); w1 &= ~(n1 * 0xFFu);
+                }
+                const f16x8 vv = kv8_f16(w0, w1);
+                if (PL == 2) o[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, plo, o[mt][t], 0, 0, 0);
+                o[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, ph, o[mt][t], 0, 0, 0);
+            }
+        }
+    }
+
+    // ---- the waves of a workgroup, in wave order ----
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        l[mt] += __shfl_xor(l[mt], 16);
+        l[mt] += __shfl_xor(l[mt], 32);
+        if (g == 0) { m_all[wave][mt * 16 + c] = m[mt]; mo_all[wave][mt * 16 + c] = mo[mt]; l_all[wave][mt * 16 + c] = l[mt]; }
+    }
+    __syncthreads();
+    float *dst = part + ((size_t)head * gridDim.y + blockIdx.y) * kv8_record(RG, HD);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        float M = -INFINITY, MO = -INFINITY, den = 0.f;
+#pragma unroll
+        for (int w = 0; w < KV8_WAVES; ++w) { M = fmaxf(M, m_all[w][mt * 16 + c]); MO = fmaxf(MO, mo_all[w][mt * 16 + c]); }
+#pragma unroll
+        for (int w = 0; w < KV8_WAVES; ++w) {
+            const float mw = m_all[w][mt * 16 + c], lw = l_all[w][mt * 16 + c];
+            den += mw == -INFINITY ? lw : kv8_exp2(mw - M) * lw;         // (lw is zero there, or NaN)
+        }
+        const float mine = mo[mt] == -INFINITY ? 1.f : kv8_exp2(mo[mt] - MO);
+        const int r = r0 + mt * 16 + c;
+        const float norm = kv8_exp2(MO - KV8_LIFT - M) / den;
+#pragma unroll
+        for (int t0 = 0; t0 < DT; t0 += CH) {
+            if (mt || t0) __syncthreads();
+#pragma unroll
+            for (int t = 0; t < CH; ++t) if (t0 + t < DT) o_slot[wave][t][lane] = o[mt][t0 + t] * mine;
+            __syncthreads();
+            for (int t = wave; t < CH && t0 + t < DT; t += KV8_WAVES) {
+                f32x4 a = o_slot[0][t][lane];
+#pragma unroll
+                for (int w = 1; w < KV8_WAVES; ++w) a += o_slot[w][t][lane];
+                const int d = (t0 + t) * 16 + g * 4;
+                if (pt.splits > 1) kv8_put(dst + (mt * 16 + c) * HD + d, make_float4(a[0], a[1], a[2], a[3]));
+                else if (r < rows) kv8_out(out + ((size_t)b * pl.L + r / pl.group) * ldo + ((size_t)head * pl.group + r % pl.group) * HD + d, a * norm, vec & 2);
+            }
+        }
+        if (pt.splits > 1 && wave == 0 && g == 0) {
+            float *e = dst + RG * HD + mt * 16 + c;
+            e[0] = M; e[RG] = MO; e[2 * RG] = den;
+        }
+    }
+}
+
+// Joins the splits of a pair, in split order.
+template <typename T>
+__global__ __launch_bounds__(256) void kv8_merge_kernel(const float *__restrict__ part, Kv8Plan pl, int hd, int slots_total, T *__restrict__ out,
+                                                        int64_t ldo, int vec)
+{
+    Kv8Part pt;
+    if (!kv8_part(pl, (int)blockIdx.y, true, pt) || pt.splits < 2) return;
+    const int head = blockIdx.x, b = pt.pair / pl.qgroups, r0 = (pt.pair - b * pl.qgroups) * pl.rg, rows = pl.L * pl.group;
+    const size_t rec = kv8_record(pl.rg, hd);
+    const float *src = part + ((size_t)head * slots_total + pt.base) * rec;
+    for (int u = threadIdx.x; u < pl.rg * hd / 4; u += 256) {
+        const int lr = u / (hd / 4), d = u % (hd / 4) * 4, r = r0 + lr;
+        if (r >= rows) continue;
+        const float *e = src + pl.rg * hd + lr;
+        float M = -INFINITY, MO = -INFINITY, den = 0.f;
+        for (int s = 0; s < pt.splits; ++s) { M = fmaxf(M, e[s * rec]); MO = fmaxf(MO, e[s * rec + pl.rg]); }
+        f32x4 a = {0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < pt.splits; ++s) {
+            const float ms = e[s * rec], mos = e[s * rec + pl.rg], ls = e[s * rec + 2 * pl.rg];
+            den += ms == -INFINITY ? ls : kv8_exp2(ms - M) * ls;
+            const float4 v = *reinterpret_cast<const float4 *>(src + s * rec + lr * hd + d);
+            a += (f32x4){v.x, v.y, v.z, v.w} * (mos == -INFINITY ? 1.f : kv8_exp2(mos - MO));
+        }
+        kv8_out(out + ((size_t)b * pl.L + r / pl.group) * ldo + ((size_t)head * pl.group + r % pl.group) * hd + d, a * (kv8_exp2(MO - KV8_LIFT - M) / den), vec & 2);
+    }
+}
+
+static int kv8_plan(int n_seqs, int L, int n_heads, int n_kv, int hd, int cap, Kv8Plan *pl, int *slots_total)
+{
+    if (!kv8_sizes(n_seqs, L, n_kv, hd, cap) || n_heads < n_kv || n_heads % n_kv || n_heads > KV8_MAX_HEADS) return SJD_EINVAL;
+    const int64_t rows = (int64_t)L * (n_heads / n_kv);
+    const int rg = rows > 16 ? 32 : 16;
+    const int64_t pairs = n_seqs * ((rows + rg - 1) / rg);
+    if (rows > INT32_MAX - 64 || pairs > 65535) return SJD_EINVAL;
+    pl->n_seqs = n_seqs; pl->L = L; pl->group = n_heads / n_kv; pl->qgroups = (int)((rows + rg - 1) / rg); pl->rg = rg;
+    pl->cap = cap; pl->nblk = (cap + 31) / 32;
+    pl->slots = pairs * n_kv >= 512 ? 0 : std::max(1, 768 / n_kv);
+    *slots_total = (int)pairs + pl->slots;
+    return SJD_OK;
+}
+
+extern "C" int sjd_kv8_attention_workspace(int32_t n_seqs, int32_t L, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t cap,
+                                           size_t *bytes)
+{
+    if (!bytes) return SJD_EINVAL;
+    Kv8Plan pl;
+    int slots;
+    SJD_TRY(kv8_plan(n_seqs, L, n_heads, n_kv_heads, head_dim, cap, &pl, &slots));
+    *bytes = pl.slots ? (size_t)slots * n_kv_heads * kv8_record(pl.rg, head_dim) * sizeof(float) : 0;
+    return SJD_OK;
+}
+
+extern "C" int sjd_kv8_attention(int32_t dtype, const void *q, int64_t ldq, const uint8_t *cache, const uint8_t *scales, const int32_t *len,
+                                 int32_t n_seqs, int32_t L, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t cap, int32_t window,
+                                 int32_t sinks, void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!q || !cache || !scales || !len || !out || (dtype != 0 && dtype != 1) || window < 0 || sinks < 0) return SJD_EINVAL;
+    if (!mx_aligned(cache) || !mx_aligned(scales)) return SJD_EINVAL;
+    size_t need = 0;
+    SJD_TRY(sjd_kv8_attention_workspace(n_seqs, L, n_heads, n_kv_heads, head_dim, cap, &need));
+    if (need && (!workspace || workspace_bytes < need || !mx_aligned(workspace))) return SJD_EINVAL;
+    if (ldq < (int64_t)n_heads * head_dim || ldo < (int64_t)n_heads * head_dim) return SJD_EINVAL;
+    Kv8Plan pl;
+    int slots;
+    SJD_TRY(kv8_plan(n_seqs, L, n_heads, n_kv_heads, head_dim, cap, &pl, &slots));
+    pl.len = len; pl.window = window; pl.sinks = sinks;
+    const int vec = (mx_vec(q, ldq, dtype) ? 1 : 0) | ((uintptr_t)out % (dtype ? 8 : 16) == 0 && ldo % 4 == 0 ? 2 : 0);
+    hipStream_t s = (hipStream_t)stream;
+    const dim3 grid(n_kv_heads, slots);
+#define GO(HD, MT, T) SJD_LAUNCH((kv8_attention_kernel<HD, MT, T>), grid, dim3(64 * KV8_WAVES), 0, s, (const T *)q, ldq, cache, scales, pl, (T *)out, ldo, vec, (float *)workspace)
+#define GO2(HD) do { if (pl.rg == 16) { if (dtype == 0) GO(HD, 1, float); else GO(HD, 1, bf16_t); } \
+                     else { if (dtype == 0) GO(HD, 2, float); else GO(HD, 2, bf16_t); } } while (0)
+    switch (head_dim) {
+        case 32: GO2(32); break;
+        case 64: GO2(64); break;
+        case 96: GO2(96); break;
+        case 128: GO2(128); break;
+        default: GO2(256); break;
+    }
+#undef GO2
+#undef GO
+    HIP_TRY(hipGetLastError());
+    if (pl.slots) {
+        const dim3 mgrid(n_kv_heads, pl.n_seqs * pl.qgroups);
+        if (dtype == 0) SJD_LAUNCH((kv8_merge_kernel<float>), mgrid, dim3(256), 0, s, (const float *)workspace, pl, head_dim, slots, (float *)out, ldo, vec);
+        else SJD_LAUNCH((kv8_merge_kernel<bf16_t>), mgrid, dim3(256), 0, s, (const float *)workspace, pl, head_dim, slots, (bf16_t *)out, ldo, vec);
+        HIP_TRY(hipGetLastError());
+    }
+    return SJD_OK;
+}

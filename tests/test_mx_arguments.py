@@ -1,0 +1,102 @@
+"""What the microscaled operators refuse, before anything reaches a GPU, and the sizes they state (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import mx_reference as R  # noqa: E402
+from paper_2410_01699_amd import binding as B  # noqa: E402
+
+OK, BAD = B.SJD_OK, B.SJD_EINVAL
+P = 1 << 20                 # an address that no refused call touches
+ODD = P + 8
+
+
+def call(name, args, **change):
+    """the C entry with the named arguments, some changed"""
+    a = dict(args, **change)
+    return getattr(B._lib, name)(*a.values())
+
+
+QUANT = dict(format=8, dtype=0, x=P, up=None, ld=64, rows=4, K=64, codes=P, scales=P, stream=None)
+NORM = dict(format=8, dtype=0, x=P, ldx=64, resid=P, ldr=64, gain=P, eps=1e-5, rows=4, d=64, codes=P, scales=P, stream=None)
+WEIGHTS = dict(dtype=0, W=P, ld=64, N=16, K=64, packed=P, stream=None)
+PRODUCT = dict(format=8, codes=P, scales=P, packed=P, M=4, N=16, K=64, dtype=0, C=P, ldc=16, ws=P, ws_bytes=1 << 30, stream=None)
+APPEND = dict(dtype=0, k=P, v=P, ld=128, len=P, n_seqs=2, L=4, n_kv=2, hd=64, cap=64, cache=P, scales=P, stream=None)
+ATTEND = dict(dtype=0, q=P, ldq=256, cache=P, scales=P, len=P, n_seqs=2, L=4, heads=4, n_kv=2, hd=64, cap=64, window=0, sinks=0, out=P, ldo=256,
+              ws=P, ws_bytes=1 << 30, stream=None)
+
+REFUSED = [
+    ("sjd_mx_quantize", QUANT, [dict(format=6), dict(dtype=2), dict(dtype=-1), dict(x=None), dict(codes=None), dict(scales=None), dict(ld=63), dict(rows=0),
+                                dict(K=0), dict(K=B.SJD_MX_MAX_K + 1, ld=1 << 40), dict(codes=ODD), dict(scales=ODD)]),
+    ("sjd_mx_rmsnorm", NORM, [dict(format=0), dict(dtype=2), dict(x=None, resid=None), dict(gain=None), dict(codes=None), dict(scales=None), dict(ldx=63),
+                              dict(ldr=63), dict(rows=0), dict(rows=-1), dict(d=0), dict(eps=-1.0), dict(eps=float("nan")), dict(codes=ODD), dict(scales=ODD)]),
+    ("sjd_mx_weights", WEIGHTS, [dict(dtype=2), dict(W=None), dict(packed=None), dict(packed=ODD), dict(ld=63), dict(N=0), dict(K=0)]),
+    ("sjd_mx_product", PRODUCT, [dict(format=5), dict(dtype=2), dict(codes=None), dict(scales=None), dict(packed=None), dict(C=None), dict(M=0), dict(N=0),
+                                 dict(K=0), dict(ldc=15), dict(codes=ODD), dict(scales=ODD), dict(packed=ODD)]),
+    ("sjd_kv8_append", APPEND, [dict(dtype=2), dict(k=None), dict(v=None), dict(len=None), dict(cache=None), dict(scales=None), dict(cache=ODD), dict(scales=ODD),
+                                dict(ld=127), dict(n_seqs=0), dict(n_seqs=1 << 20), dict(L=0), dict(L=65), dict(n_kv=0), dict(n_kv=1 << 20, ld=1 << 40), dict(hd=48),
+                                dict(hd=0), dict(hd=512, ld=2048), dict(cap=0), dict(cap=2 ** 31 - 1)]),
+    ("sjd_kv8_attention", ATTEND, [dict(dtype=2), dict(q=None), dict(cache=None), dict(scales=None), dict(len=None), dict(out=None), dict(cache=ODD),
+                                   dict(scales=ODD), dict(ldq=255), dict(ldo=255), dict(n_seqs=0), dict(L=0), dict(L=65), dict(heads=3), dict(heads=1),
+                                   dict(heads=0), dict(hd=80), dict(cap=0), dict(window=-1), dict(sinks=-1), dict(ws=None), dict(ws=ODD), dict(ws_bytes=16)]),
+]
+
+
+@pytest.mark.parametrize("name,args,change", [(n, a, c) for n, a, cs in REFUSED for c in cs], ids=lambda v: v if isinstance(v, str) else "-".join(v) if len(v) < 4 else "")
+def test_the_entry_refuses(name, args, change):
+    assert call(name, args, **change) == BAD
+
+
+def test_sizes():
+    assert B.sjd_mx_weights_bytes(1, 1) == 4352 and B.sjd_mx_weights_bytes(17, 513) == 4 * 4352
+    assert B.sjd_mx_weights_bytes(22016, 4096) == 1376 * 8 * 4352
+    n = C.c_size_t()
+    for f, bad in (("sjd_mx_weights_bytes", (0, 1)), ("sjd_mx_weights_bytes", (1, 0)), ("sjd_mx_product_workspace", (0, 1, 1)),
+                   ("sjd_kv8_attention_workspace", (1, 1, 3, 2, 64, 64)), ("sjd_kv8_attention_workspace", (1, 1, 2, 2, 48, 64))):
+        assert getattr(B._lib, f)(*bad, C.byref(n)) == BAD
+    assert B._lib.sjd_mx_weights_bytes(1, 1, None) == BAD and B._lib.sjd_mx_product_workspace(1, 1, 1, None) == BAD
+    assert B._lib.sjd_kv8_attention_workspace(1, 1, 1, 1, 64, 64, None) == BAD
+    # a workspace does not depend on how long the cache is
+    assert B.sjd_kv8_attention_workspace(1, 1, 8, 8, 128, 1 << 20) == B.sjd_kv8_attention_workspace(1, 1, 8, 8, 128, 64)
+
+
+def u8(n):
+    return torch.empty(n, dtype=torch.uint8)
+
+
+def test_the_binding_refuses_what_is_not_on_the_gpu():
+    x = torch.empty(2, 64)
+    for f in (lambda: B.sjd_mx_quantize(8, x, u8(256), u8(8)),
+              lambda: B.sjd_mx_rmsnorm(8, x, None, torch.empty(64), 1e-5, u8(256), u8(8)),
+              lambda: B.sjd_mx_rmsnorm(8, None, None, torch.empty(64), 1e-5, u8(256), u8(8)),
+              lambda: B.sjd_mx_weights(x, u8(4352)),
+              lambda: B.sjd_mx_product(8, u8(256), u8(8), u8(4352), 64, torch.empty(2, 16), None),
+              lambda: B.sjd_kv8_append(x, x, torch.zeros(2, dtype=torch.int32), 1, 1, 64, 32, u8(8192), u8(4)),
+              lambda: B.sjd_kv8_attention(x, u8(8192), u8(4), torch.zeros(2, dtype=torch.int32), 1, 1, 1, 64, 32, 0, 0, x, None)):
+        with pytest.raises(B.SjdError) as e:
+            f()
+        assert e.value.code == BAD
+
+
+def test_formats_of_the_reference():
+    """the tables, rounding and scales that the GPU tests compare with, against torch's own E4M3 and by hand"""
+    t = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()
+    assert ((t == R.table(8)) | (t != t)).all() and R.table(4)[:8].tolist() == [0, 0.5, 1, 1.5, 2, 3, 4, 6]
+    x = torch.cat((torch.linspace(-448, 448, 20011), torch.linspace(-0.1, 0.1, 20011), torch.tensor([17.0, 19.0, 0.0009765625])))
+    assert (R.nearest(x.double().numpy(), 8) == x.to(torch.float8_e4m3fn).view(torch.uint8).numpy()).all()
+    assert [int(R.nearest(torch.tensor([v]).double().numpy(), 4)[0]) for v in (0.25, 0.26, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 5.1, -5.1)] == [0, 1, 2, 2, 4, 4, 6, 6, 7, 15]
+    for a, b8 in ((448.0, 127), (448.5, 128), (224.0, 126), (1.0, 119), (0.0, 0), (2.0 ** -149, 0)):
+        assert R.scale_byte(a, 8) == b8 == int(R.scale_bytes(torch.tensor([a]).double().numpy(), 8)[0])
+
+
+def test_packed_orders_hold_every_value_once():
+    k, v = R.cache_at(96)
+    assert sorted(k.reshape(-1).tolist() + v.reshape(-1).tolist()) == list(range(64 * 96))
+    import numpy as np
+    codes = np.random.RandomState(0).randint(0, 16, (21, 640)).astype(np.uint8)
+    scales = np.random.RandomState(1).randint(1, 255, (21, 20)).astype(np.uint8)
+    w = R.pack_weights(codes, scales, 21, 640).reshape(2, 2, 4352)
+    n, kk = 19, 513 + 128 + 64 + 3 - 130                     # feature 19, value 578: group 1, step 0, quarter 2, value 2 of it
+    assert kk == 578 and w[1, 1, 16 * (16 * 2 + 3) + 1] & 15 == codes[n, kk] and w[1, 1, 4096 + 4 * (16 * 2 + 3)] == scales[n, 18]
