@@ -7,6 +7,7 @@ Importing this module raises if the library has not been built: there is no fall
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -360,68 +361,106 @@ def sjd_gemm_bench(M, N, K, tn, wk, u, iters=50) -> float:
 
 # ---- microscaled operators ------------------------------------------------------------------------
 # Matrices may be rows of wider ones (last dimension contiguous); everything else is contiguous.  A tensor that is on another
-# device than the current one, or too small for what the call reads or writes, is refused.
-def _need(ok, what):
-    if not ok:
-        raise SjdError(SJD_EINVAL, what)
+# device than the current one, or too small for what the call reads or writes, is refused.  Kernels of a few us wait for
+# these checks, so they are plain comparisons and pass addresses as numbers.
+_KINDS = {}         # torch's types: the dtype code of fp32 and bf16
 
 
-def _here(name, t, dtypes):
+def _refuse(what):
+    raise SjdError(SJD_EINVAL, what)
+
+
+def _device(t):
+    """the current device, on which t has to be"""
     import torch
-    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{name} is not on the current device")
-    _need(str(t.dtype)[6:] in dtypes, f"{name} is {t.dtype}, not {' or '.join(dtypes)}")
-    return t
+    if not _KINDS:
+        _KINDS.update({torch.float32: 0, torch.bfloat16: 1, torch.uint8: "uint8", torch.int32: "int32"})
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        _refuse(f"a tensor is on {t.device}, which is not the current GPU")
+    return dev
 
 
-def _rows(name, t, rows, cols, dtypes=("float32", "bfloat16")):
-    """(address, dtype code, elements from row to row) of a [rows, cols] matrix; None -> NULL"""
-    if t is None:
-        return None, 0, 0
-    _here(name, t, dtypes)
-    _need(tuple(t.shape) == (rows, cols), f"{name} is {tuple(t.shape)}, not {(rows, cols)}")
-    _need((cols == 1 or t.stride(1) == 1) and (rows == 1 or t.stride(0) >= cols), f"{name}: rows are not contiguous, or overlap")
-    return C.c_void_p(t.data_ptr()), int(t.dtype.itemsize == 2), cols if rows == 1 else t.stride(0)
+def _rows(dev, name, t, rows, cols):
+    """(address, dtype code, elements from row to row) of a [rows, cols] matrix"""
+    code = _KINDS.get(t.dtype)
+    if t.get_device() != dev or (code != 0 and code != 1):
+        _refuse(f"{name} is {t.dtype} on {t.device}: float32 or bfloat16 on the current device is needed")
+    if t.shape != (rows, cols):
+        _refuse(f"{name} is {tuple(t.shape)}, not {(rows, cols)}")
+    ld, step = t.stride()
+    if rows == 1:
+        ld = cols
+    if (step != 1 and cols > 1) or ld < cols:
+        _refuse(f"{name}: rows are not contiguous, or overlap")
+    return t.data_ptr(), code, ld
 
 
-def _flat(name, t, count, dtype="uint8", exact=True):
-    """address of a contiguous tensor of `count` elements (or at least as many)"""
-    _here(name, t, (dtype,))
-    _need(t.is_contiguous() and (t.numel() == count if exact else t.numel() >= count), f"{name}: {count} contiguous elements are needed, got {tuple(t.shape)}")
-    return C.c_void_p(t.data_ptr())
+def _flat(dev, name, t, count, kind="uint8", more=False):
+    """address of a contiguous tensor of `count` elements (more: or of more)"""
+    if t.get_device() != dev or _KINDS.get(t.dtype) != kind:
+        _refuse(f"{name} is {t.dtype} on {t.device}: another type, or not the current device")
+    if not t.is_contiguous() or (t.numel() < count if more else t.numel() != count):
+        _refuse(f"{name}: {count} contiguous elements are needed, got {tuple(t.shape)}")
+    return t.data_ptr()
 
 
-def _coded(format, rows, K, codes, scales):
+def _coded(dev, format, rows, K, codes, scales):
     """addresses of a matrix's codes and scales"""
-    _need(format in (SJD_MX8, SJD_MX4), "format is SJD_MX8 or SJD_MX4")
-    Kp = -(-K // 128) * 128
-    return _flat("codes", codes, rows * Kp * format // 8), _flat("scales", scales, rows * Kp // 32)
+    if format != SJD_MX8 and format != SJD_MX4:
+        _refuse("format is SJD_MX8 or SJD_MX4")
+    Kp = (K + 127) // 128 * 128
+    return _flat(dev, "codes", codes, rows * Kp * format // 8), _flat(dev, "scales", scales, rows * Kp // 32)
 
 
-def _workspace(workspace, need):
-    return (None, 0) if not need else (_flat("workspace", workspace, need, exact=False), workspace.numel())
+def _workspace(dev, workspace, need):
+    return (_flat(dev, "workspace", workspace, need, more=True), workspace.numel()) if need else (None, 0)
+
+
+def _matrix(name, t):
+    if t.dim() != 2:
+        _refuse(f"{name} is a matrix")
+    return t.shape
+
+
+def _on(stream):
+    return None if stream is None else stream.cuda_stream
+
+
+def _done(rc):
+    if rc:
+        _check(rc)
 
 
 def sjd_mx_quantize(format, x, codes, scales, up=None, stream=None):
     """x: device [rows, K] (up: the same, then of SiLU(x) * up) -> codes, scales"""
-    _need(x.dim() == 2, "x is a matrix")
-    rows, K = x.shape
-    px, dt, ld = _rows("x", x, rows, K)
-    pu, du, lu = _rows("up", up, rows, K)
-    _need(up is None or (du == dt and lu == ld), "x and up have the same type and stride")
-    _check(_lib.sjd_mx_quantize(format, dt, px, pu, ld, rows, K, *_coded(format, rows, K, codes, scales), _stream(stream)))
+    dev = _device(x)
+    rows, K = _matrix("x", x)
+    px, dt, ld = _rows(dev, "x", x, rows, K)
+    pu = None
+    if up is not None:
+        pu, du, lu = _rows(dev, "up", up, rows, K)
+        if du != dt or lu != ld:
+            _refuse("x and up have the same type and stride")
+    pc, ps = _coded(dev, format, rows, K, codes, scales)
+    _done(_lib.sjd_mx_quantize(format, dt, px, pu, ld, rows, K, pc, ps, _on(stream)))
 
 
 def sjd_mx_rmsnorm(format, x, resid, gain, eps, codes, scales, stream=None):
     """x [rows, d] (or None) added to resid fp32 [rows, d] (in place; or None), normalised -> codes, scales"""
-    of = x if x is not None else resid
-    _need(of is not None and of.dim() == 2, "x or resid is a matrix")
-    rows, d = of.shape
-    px, dt, ldx = _rows("x", x, rows, d)
-    pr, _, ldr = _rows("resid", resid, rows, d, ("float32",))
-    _check(_lib.sjd_mx_rmsnorm(format, dt, px, ldx, pr, ldr, _flat("gain", gain, d, "float32"), eps, rows, d,
-                               *_coded(format, rows, d, codes, scales), _stream(stream)))
+    if x is None and resid is None:
+        _refuse("x or resid is a matrix")
+    dev = _device(gain)
+    rows, d = _matrix("x", x) if x is not None else _matrix("resid", resid)
+    px, dt, ldx = (None, 0, 0) if x is None else _rows(dev, "x", x, rows, d)
+    pr, dr, ldr = (None, 0, 0) if resid is None else _rows(dev, "resid", resid, rows, d)
+    if dr:
+        _refuse("resid is float32")
+    pc, ps = _coded(dev, format, rows, d, codes, scales)
+    _done(_lib.sjd_mx_rmsnorm(format, dt, px, ldx, pr, ldr, _flat(dev, "gain", gain, d, 0), eps, rows, d, pc, ps, _on(stream)))
 
 
+@functools.lru_cache(maxsize=4096)
 def sjd_mx_weights_bytes(N, K) -> int:
     n = _sz(0)
     _check(_lib.sjd_mx_weights_bytes(N, K, C.byref(n)))
@@ -430,12 +469,13 @@ def sjd_mx_weights_bytes(N, K) -> int:
 
 def sjd_mx_weights(W, packed, stream=None):
     """W: device [N, K] -> packed: device uint8, sjd_mx_weights_bytes(N, K) of them"""
-    _need(W.dim() == 2, "W is a matrix")
-    N, K = W.shape
-    pw, dt, ld = _rows("W", W, N, K)
-    _check(_lib.sjd_mx_weights(dt, pw, ld, N, K, _flat("packed", packed, sjd_mx_weights_bytes(N, K)), _stream(stream)))
+    dev = _device(W)
+    N, K = _matrix("W", W)
+    pw, dt, ld = _rows(dev, "W", W, N, K)
+    _done(_lib.sjd_mx_weights(dt, pw, ld, N, K, _flat(dev, "packed", packed, sjd_mx_weights_bytes(N, K)), _on(stream)))
 
 
+@functools.lru_cache(maxsize=4096)
 def sjd_mx_product_workspace(M, N, K) -> int:
     n = _sz(0)
     _check(_lib.sjd_mx_product_workspace(M, N, K, C.byref(n)))
@@ -444,28 +484,33 @@ def sjd_mx_product_workspace(M, N, K) -> int:
 
 def sjd_mx_product(format, codes, scales, packed, K, out, workspace, stream=None):
     """out [M, N] = the rows behind codes and scales (K values each) times the packed weights"""
-    _need(out.dim() == 2, "out is a matrix")
-    M, N = out.shape
-    po, dt, ld = _rows("out", out, M, N)
-    _check(_lib.sjd_mx_product(format, *_coded(format, M, K, codes, scales), _flat("packed", packed, sjd_mx_weights_bytes(N, K)), M, N, K,
-                               dt, po, ld, *_workspace(workspace, sjd_mx_product_workspace(M, N, K)), _stream(stream)))
+    dev = _device(out)
+    M, N = _matrix("out", out)
+    po, dt, ld = _rows(dev, "out", out, M, N)
+    pc, ps = _coded(dev, format, M, K, codes, scales)
+    pw = _flat(dev, "packed", packed, sjd_mx_weights_bytes(N, K))
+    ws, ws_bytes = _workspace(dev, workspace, sjd_mx_product_workspace(M, N, K))
+    _done(_lib.sjd_mx_product(format, pc, ps, pw, M, N, K, dt, po, ld, ws, ws_bytes, _on(stream)))
 
 
-def _kv8(cache, scales, n_seqs, n_kv, hd, cap):
-    blocks = n_seqs * n_kv * -(-cap // 32)
-    return _flat("cache", cache, blocks * 64 * hd), _flat("scales", scales, blocks * 2)
+def _kv8(dev, cache, scales, n_seqs, n_kv, hd, cap):
+    blocks = n_seqs * n_kv * ((cap + 31) // 32)
+    return _flat(dev, "cache", cache, blocks * 64 * hd), _flat(dev, "scales", scales, blocks * 2)
 
 
 def sjd_kv8_append(k, v, length, L, n_kv, hd, cap, cache, scales, stream=None):
     """k, v: device [n_seqs * L, n_kv * hd]; length: device int32 [n_seqs]"""
+    dev = _device(length)
     n_seqs = length.numel()
-    pk, dt, ld = _rows("k", k, n_seqs * L, n_kv * hd)
-    pv, dv, lv = _rows("v", v, n_seqs * L, n_kv * hd)
-    _need(dt == dv and ld == lv, "k and v have the same type and stride")
-    _check(_lib.sjd_kv8_append(dt, pk, pv, ld, _flat("length", length, n_seqs, "int32"), n_seqs, L, n_kv, hd, cap,
-                               *_kv8(cache, scales, n_seqs, n_kv, hd, cap), _stream(stream)))
+    pk, dt, ld = _rows(dev, "k", k, n_seqs * L, n_kv * hd)
+    pv, dv, lv = _rows(dev, "v", v, n_seqs * L, n_kv * hd)
+    if dt != dv or ld != lv:
+        _refuse("k and v have the same type and stride")
+    pc, ps = _kv8(dev, cache, scales, n_seqs, n_kv, hd, cap)
+    _done(_lib.sjd_kv8_append(dt, pk, pv, ld, _flat(dev, "length", length, n_seqs, "int32"), n_seqs, L, n_kv, hd, cap, pc, ps, _on(stream)))
 
 
+@functools.lru_cache(maxsize=4096)
 def sjd_kv8_attention_workspace(n_seqs, L, n_heads, n_kv, hd, cap) -> int:
     n = _sz(0)
     _check(_lib.sjd_kv8_attention_workspace(n_seqs, L, n_heads, n_kv, hd, cap, C.byref(n)))
@@ -474,10 +519,13 @@ def sjd_kv8_attention_workspace(n_seqs, L, n_heads, n_kv, hd, cap) -> int:
 
 def sjd_kv8_attention(q, cache, scales, length, L, n_heads, n_kv, hd, cap, window, sinks, out, workspace, stream=None):
     """q, out: device [n_seqs * L, n_heads * hd] of one type; window 0: everything up to the query's position"""
+    dev = _device(length)
     n_seqs = length.numel()
-    pq, dt, ldq = _rows("q", q, n_seqs * L, n_heads * hd)
-    po, do, ldo = _rows("out", out, n_seqs * L, n_heads * hd)
-    _need(dt == do, "q and out have the same type")
-    need = sjd_kv8_attention_workspace(n_seqs, L, n_heads, n_kv, hd, cap)
-    _check(_lib.sjd_kv8_attention(dt, pq, ldq, *_kv8(cache, scales, n_seqs, n_kv, hd, cap), _flat("length", length, n_seqs, "int32"), n_seqs, L,
-                                  n_heads, n_kv, hd, cap, window, sinks, po, ldo, *_workspace(workspace, need), _stream(stream)))
+    pq, dt, ldq = _rows(dev, "q", q, n_seqs * L, n_heads * hd)
+    po, do, ldo = _rows(dev, "out", out, n_seqs * L, n_heads * hd)
+    if dt != do:
+        _refuse("q and out have the same type")
+    pc, ps = _kv8(dev, cache, scales, n_seqs, n_kv, hd, cap)
+    ws, ws_bytes = _workspace(dev, workspace, sjd_kv8_attention_workspace(n_seqs, L, n_heads, n_kv, hd, cap))
+    _done(_lib.sjd_kv8_attention(dt, pq, ldq, pc, ps, _flat(dev, "length", length, n_seqs, "int32"), n_seqs, L, n_heads, n_kv, hd, cap, window, sinks,
+                                 po, ldo, ws, ws_bytes, _on(stream)))

@@ -6,6 +6,7 @@
 #include "sjd_mx.h"
 
 #include <algorithm>
+#include <type_traits>
 
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
@@ -119,6 +120,9 @@ extern "C" int sjd_kv8_append(int32_t dtype, const void *k, const void *v, int64
 }
 
 // ---- attention ------------------------------------------------------------------------------
+#define KV8_WAVES 8
+#define KV8_LIFT 14      // probabilities times 2^14 in fp16: 22 bits of hi + lo hold from 2^-27 of the largest on
+
 // The queries of one sequence that read one cache head, L * (heads per cache head) rows with a query's heads next to each other, are cut
 // into groups of 16 or 32 rows.  A (sequence, group) pair walks the blocks that any of its queries sees, the sinks' first.  Where the
 // pairs are too few for the chip their walks are cut into splits, all of about the same number of blocks: lengths live on the device,
@@ -148,36 +152,37 @@ __device__ __forceinline__ Kv8Span kv8_span(const Kv8Plan &pl, int pair)
     return s;
 }
 struct Kv8Part { int32_t pair, split, splits, per, base; };     // a slot's pair, its place among the pair's splits, blocks per split
-// lanes look at 64 pairs at a time; by_pair: the part that starts the given pair, else the part of the given slot
+// Lanes look at 64 pairs at a time; by_pair: the part that starts the given pair, else the part of the given slot.  With `per` blocks
+// a split, per >= total / slots up to the rounding of fp32, the splits of all pairs are at most total / per + pairs (1 - 1 / per): never more
+// than slots + pairs.
 __device__ __forceinline__ bool kv8_part(const Kv8Plan &pl, int want, bool by_pair, Kv8Part &part)
 {
     const int pairs = pl.n_seqs * pl.qgroups, lane = threadIdx.x & 63;
-    int64_t total = 0;
+    const int c0 = lane < pairs ? kv8_span(pl, lane).count : 0;
+    float total = 0.f;
     for (int p0 = 0; p0 < pairs; p0 += 64) {
-        int64_t c = p0 + lane < pairs ? kv8_span(pl, p0 + lane).count : 0;
-#pragma unroll
-        for (int o = 32; o; o >>= 1) c += __shfl_xor(c, o);
-        total += c;
+        float c = (float)(p0 == 0 ? c0 : p0 + lane < pairs ? kv8_span(pl, p0 + lane).count : 0);
+        for (int o = 1; o < min(pairs, 64); o <<= 1) c += __shfl_xor(c, o);
+        total += __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(c)));
     }
-    part.per = max(4, (int)((total + pl.slots - 1) / pl.slots));
+    part.per = max(KV8_WAVES, (int)ceilf(total / (float)pl.slots));
     int base = 0;
     for (int p0 = 0; p0 < pairs; p0 += 64) {
-        const int c = p0 + lane < pairs ? kv8_span(pl, p0 + lane).count : 0;
+        const int c = p0 == 0 ? c0 : p0 + lane < pairs ? kv8_span(pl, p0 + lane).count : 0;
         const int mine = (c + part.per - 1) / part.per;
         int incl = mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) { const int up = __shfl_up(incl, o); if (lane >= o) incl += up; }
+        for (int o = 1; o < min(pairs, 64); o <<= 1) { const int up = __shfl_up(incl, o); if (lane >= o) incl += up; }
         const int start = base + incl - mine;
         const uint64_t hit = by_pair ? __ballot(p0 + lane == want) : __ballot(want >= start && want < start + mine);
         if (hit) {
             const int l = __ffsll((unsigned long long)hit) - 1;
             part.pair = p0 + l;
-            part.splits = __shfl(mine, l);
-            part.base = __shfl(start, l);
+            part.splits = __builtin_amdgcn_readlane(mine, l);
+            part.base = __builtin_amdgcn_readlane(start, l);
             part.split = by_pair ? 0 : want - part.base;
             return true;
         }
-        base += __shfl(incl, 63);
+        base += __builtin_amdgcn_readlane(incl, 63);
     }
     return false;
 }
@@ -190,11 +195,17 @@ __device__ __forceinline__ f16x8 kv8_f16(uint32_t lo, uint32_t hi)        // eig
 }
 // bytes 0x80 where a code is NaN (0x7F with any sign)
 __device__ __forceinline__ uint32_t kv8_nan(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
+// the largest over the four lanes of a column (l % 16)
+__device__ __forceinline__ float kv8_across(float x)
+{
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
 __device__ __forceinline__ float kv8_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ void kv8_put(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
 
-#define KV8_WAVES 4
-#define KV8_LIFT 14      // probabilities times 2^14 in fp16: 22 bits of hi + lo hold from 2^-27 of the largest on
 // record of a split: O[rg][HD] in units of 2^(mo - KV8_LIFT), then m[rg], mo[rg], l[rg]
 __host__ __device__ __forceinline__ size_t kv8_record(int rg, int hd) { return (size_t)rg * (hd + 3); }
 
@@ -219,9 +230,9 @@ __device__ __forceinline__ void kv8_out(bf16_t *p, const f32x4 &v, bool vec)
 // scales are, and fp16 holds what matters beside it.  out = O * 2^(mo - LIFT - m) / l.
 // The two score tiles of a block leave lane (g, c) with row c and the positions 16 h + 4 g + i: the order in which V's operands hold them.
 template <int HD, int MT, typename T>
-__global__ __launch_bounds__(64 * KV8_WAVES) void kv8_attention_kernel(const T *__restrict__ q, int64_t ldq, const uint8_t *__restrict__ cache,
-                                                                       const uint8_t *__restrict__ scales, Kv8Plan pl, T *__restrict__ out,
-                                                                       int64_t ldo, int vec, float *__restrict__ part)
+__global__ __launch_bounds__(64 * KV8_WAVES, MT == 1 && HD <= 128 ? 4 : 2) void kv8_attention_kernel(const T *__restrict__ q, int64_t ldq, const uint8_t *__restrict__ cache,
+                                                                          const uint8_t *__restrict__ scales, Kv8Plan pl, T *__restrict__ out,
+                                                                          int64_t ldo, int vec, float *__restrict__ part)
 {
     constexpr int KS = HD / 32, DT = HD / 16, RG = MT * 16, PL = sizeof(T) == 4 ? 2 : 1, CH = DT < 8 ? DT : 8;
     __shared__ f16x8 q_lds[MT][KS][PL][64];
@@ -238,12 +249,32 @@ __global__ __launch_bounds__(64 * KV8_WAVES) void kv8_attention_kernel(const T *
     const int v_beg = pt.split * per, v_end = min(sp.count, v_beg + per);
     const int b = pt.pair / pl.qgroups, r0 = (pt.pair - b * pl.qgroups) * RG, rows = pl.L * pl.group;
 
+    // The next block's keys are requested when this block's have left their registers, its values likewise.
+    const size_t at0 = ((size_t)b * heads + head) * pl.nblk;
+    uint4 ka[KS], va[KS];
+    int sc = 0;
+    auto place = [&](int v) { return v < sp.front ? v : sp.first + v - sp.front; };
+    auto fetch_k = [&](int blk) {
+        const uint4 *rec = reinterpret_cast<const uint4 *>(cache + (at0 + blk) * (64 * HD)) + lane;
+#pragma unroll
+        for (int p = 0; p < KS; ++p) ka[p] = rec[p * 64];
+        sc = *reinterpret_cast<const uint16_t *>(scales + (at0 + blk) * 2);
+    };
+    auto fetch_v = [&](int blk) {
+        const uint4 *rec = reinterpret_cast<const uint4 *>(cache + (at0 + blk) * (64 * HD)) + lane;
+#pragma unroll
+        for (int p = 0; p < KS; ++p) va[p] = rec[(KS + p) * 64];
+    };
+    int v = v_beg + wave;
+    if (v < v_end) { fetch_k(place(v)); fetch_v(place(v)); }
+    __builtin_amdgcn_sched_barrier(0);
+
     // Q of row tile mt by wave mt: lane (g, c) has values 32 ks + 8 g .. of row c
-    if (wave < MT) {
-        const int r = r0 + wave * 16 + c;
+    for (int mt = wave; mt < MT; mt += KV8_WAVES) {
+        const int r = min(r0 + mt * 16 + c, rows - 1);
         float x[KS][8];
         uint32_t top = 0;
-        const T *src = q + ((size_t)b * pl.L + min(r, rows - 1) / pl.group) * ldq + ((size_t)head * pl.group + min(r, rows - 1) % pl.group) * HD;
+        const T *src = q + ((size_t)b * pl.L + r / pl.group) * ldq + ((size_t)head * pl.group + r % pl.group) * HD;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             mx_load8<T>(src, ks * 32 + g * 8, HD, vec & 1, x[ks]);
@@ -259,14 +290,14 @@ __global__ __launch_bounds__(64 * KV8_WAVES) void kv8_attention_kernel(const T *
             f16x8 hi, lo;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float y = x[ks][e] * mul;
+                const float y = x[ks][e] * mul;              // (exact)
                 hi[e] = (_Float16)y;
                 lo[e] = (_Float16)(y - (float)hi[e]);
             }
-            q_lds[wave][ks][0][lane] = hi;
-            if (PL == 2) q_lds[wave][ks][PL - 1][lane] = lo;
+            q_lds[mt][ks][0][lane] = hi;
+            if (PL == 2) q_lds[mt][ks][PL - 1][lane] = lo;
         }
-        if (g == 0) q_scale[wave * 16 + c] = mx_pow2(127 - up) * (1.4426950408889634f / sqrtf((float)HD));
+        if (g == 0) q_scale[mt * 16 + c] = mx_pow2(127 - up) * (1.4426950408889634f / sqrtf((float)HD));
     }
     __syncthreads();
 
@@ -281,17 +312,10 @@ __global__ __launch_bounds__(64 * KV8_WAVES) void kv8_attention_kernel(const T *
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[mt][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
-    const size_t at0 = ((size_t)b * heads + head) * pl.nblk;
-    for (int v = v_beg + wave; v < v_end; v += KV8_WAVES) {
-        const int blk = v < sp.front ? v : sp.first + v - sp.front, k0 = blk * 32;
-        const uint4 *rec = reinterpret_cast<const uint4 *>(cache + (at0 + blk) * (64 * HD)) + lane;
-        uint4 ka[KS], va[KS];
-#pragma unroll
-        for (int p = 0; p < KS; ++p) ka[p] = rec[p * 64];
-#pragma unroll
-        for (int p = 0; p < KS; ++p) va[p] = rec[(KS + p) * 64];
-        const int sc = *reinterpret_cast<const uint16_t *>(scales + (at0 + blk) * 2);
-        const float ks2 = mx_pow2(sc & 255), ev = (float)((sc >> 8) - 127);
+    auto block = [&](auto more) {
+        const int blk = place(v), k0 = blk * 32, next = more.value ? place(v + KV8_WAVES) : 0;
+        const int sb = __builtin_amdgcn_readfirstlane(sc);
+        const float ks2 = mx_pow2(sb & 255), ev = (float)((sb >> 8) - 127);
         const bool whole = k0 + 31 <= sp.n + sp.i0 && (!pl.window || k0 > sp.n + sp.i1 - pl.window || k0 + 31 < pl.sinks);
         f32x4 s[MT][2];
 #pragma unroll
@@ -306,67 +330,106 @@ __global__ __launch_bounds__(64 * KV8_WAVES) void kv8_attention_kernel(const T *
                 for (int p = PL - 1; p >= 0; --p) s[mt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q_lds[mt][ks][p][lane], s[mt][h], 0, 0, 0);
             }
         }
-        bool nan = false;
-        if (!whole) {                         // NaN among values that a mask hides from some row
-            uint32_t any = 0;
-#pragma unroll
-            for (int p = 0; p < KS; ++p) any |= kv8_nan(va[p].x) | kv8_nan(va[p].y) | kv8_nan(va[p].z) | kv8_nan(va[p].w);
-            nan = __ballot(any != 0) != 0;
-        }
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (more.value) { fetch_k(next); __builtin_amdgcn_sched_barrier(0); }
+        f16x8 ph[MT], plo[MT];
+        uint32_t seen[MT];
+        float turn[MT];                          // what a row's output so far is rescaled by
+        bool turns = false;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            float x[8], bm = -INFINITY;
-            bool see[8];
             const float cs = qs[mt] * ks2;
+            float x[8], bm;
+            seen[mt] = 0xFFu;
+            if (whole) {
+                bm = s[mt][0][0];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int key = k0 + (e >> 2) * 16 + g * 4 + (e & 3);
-                see[e] = whole || (key <= pos[mt] && (!pl.window || key > pos[mt] - pl.window || key < pl.sinks));
-                x[e] = see[e] ? s[mt][e >> 2][e & 3] * cs : -INFINITY;
-                bm = fmaxf(bm, x[e]);
+                for (int e = 1; e < 8; ++e) bm = fmaxf(bm, s[mt][e >> 2][e & 3]);
+                bm *= cs;
+            } else {
+                bm = -INFINITY;
+                seen[mt] = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int key = k0 + (e >> 2) * 16 + g * 4 + (e & 3);
+                    const bool see = key <= pos[mt] && (!pl.window || key > pos[mt] - pl.window || key < pl.sinks);
+                    seen[mt] |= see ? 1u << e : 0u;
+                    x[e] = see ? s[mt][e >> 2][e & 3] * cs : -INFINITY;
+                    bm = fmaxf(bm, x[e]);
+                }
             }
-            bm = fmaxf(bm, __shfl_xor(bm, 16));
-            bm = fmaxf(bm, __shfl_xor(bm, 32));
+            bm = kv8_across(bm);
             const float mn = fmaxf(m[mt], bm), mon = fmaxf(mo[mt], bm + ev);
-            const float so = mn == -INFINITY ? 1.f : kv8_exp2(m[mt] - mn), soo = mon == -INFINITY ? 1.f : kv8_exp2(mo[mt] - mon);
+            const float so = mn == -INFINITY ? 1.f : kv8_exp2(m[mt] - mn);
             const float f = mn == -INFINITY ? 0.f : kv8_exp2(fminf(ev - mon + mn + KV8_LIFT, 120.f));
+            turn[mt] = mon == -INFINITY ? 1.f : kv8_exp2(mo[mt] - mon);
+            turns |= turn[mt] != 1.f;
+            if (whole) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = kv8_exp2(fmaf(s[mt][e >> 2][e & 3], cs, -mn));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = seen[mt] >> e & 1 ? kv8_exp2(x[e] - mn) : 0.f;
+            }
             float sum = 0.f;
-            f16x8 ph, plo;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float p = see[e] ? kv8_exp2(x[e] - mn) : 0.f;
-                sum += p;
-                float pf = p * f;
-                asm("" : "+v"(pf));          // (the product in fp32 for both parts: fused into the conversion to fp16 it rounds otherwise now and then)
-                ph[e] = (_Float16)pf;
-                plo[e] = (_Float16)(pf - (float)ph[e]);
+                sum += x[e];
+                float pf = x[e] * f;
+                if (PL == 2) asm("" : "+v"(pf));     // (the product in fp32 for both parts: fused into the conversion to fp16 it rounds otherwise now and then)
+                ph[mt][e] = (_Float16)pf;
+                if (PL == 2) plo[mt][e] = (_Float16)(pf - (float)ph[mt][e]);
             }
             l[mt] = l[mt] * so + sum;
             m[mt] = mn; mo[mt] = mon;
+        }
+        if (__ballot(turns)) {                   // (rare once a row has met its largest scores)
 #pragma unroll
-            for (int t = 0; t < DT; ++t) {
-                uint32_t w0 = (t & 1) ? va[t / 2].z : va[t / 2].x, w1 = (t & 1) ? va[t / 2].w : va[t / 2].y;
-                o[mt][t] *= soo;
-                if (nan) {
-                    // zero times NaN is NaN: NaN codes are taken out, and the rows that see one get it by counting
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int t = 0; t < DT; ++t) o[mt][t] *= turn[mt];
+        }
+        if (!whole) {
+            // Zero times NaN is NaN: where a mask may hide a NaN code from some row, the codes are taken out, and the rows that see one
+            // get it by counting.
+            uint32_t any = 0;
+#pragma unroll
+            for (int p = 0; p < KS; ++p) any |= kv8_nan(va[p].x) | kv8_nan(va[p].y) | kv8_nan(va[p].z) | kv8_nan(va[p].w);
+            if (__ballot(any != 0)) {
+#pragma unroll
+                for (int t = 0; t < DT; ++t) {
+                    uint32_t &w0 = (t & 1) ? va[t / 2].z : va[t / 2].x, &w1 = (t & 1) ? va[t / 2].w : va[t / 2].y;
                     const uint32_t n0 = kv8_nan(w0) >> 7, n1 = kv8_nan(w1) >> 7;        // 1 in the byte of a NaN
                     f16x8 ind, vis;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        ind[e] = (_Float16)(float)(((e < 4 ? n0 : n1) >> (8 * (e & 3))) & 1u);
-                        vis[e] = see[e] ? (_Float16)1.f : (_Float16)0.f;
-                    }
-                    f32x4 hits = {0.f, 0.f, 0.f, 0.f};
-                    hits = __builtin_amdgcn_mfma_f32_16x16x32_f16(ind, vis, hits, 0, 0, 0);
+                    for (int e = 0; e < 8; ++e) ind[e] = (_Float16)(float)(((e < 4 ? n0 : n1) >> (8 * (e & 3))) & 1u);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) if (hits[i] != 0.f) o[mt][t][i] = NAN;
+                    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) vis[e] = (_Float16)(float)(seen[mt] >> e & 1u);
+                        f32x4 hits = {0.f, 0.f, 0.f, 0.f};
+                        hits = __builtin_amdgcn_mfma_f32_16x16x32_f16(ind, vis, hits, 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) if (hits[i] != 0.f) o[mt][t][i] = NAN;
+                    }
                     w0 &= ~(n0 * 0xFFu); w1 &= ~(n1 * 0xFFu);
                 }
-                const f16x8 vv = kv8_f16(w0, w1);
-                if (PL == 2) o[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, plo, o[mt][t], 0, 0, 0);
-                o[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, ph, o[mt][t], 0, 0, 0);
             }
         }
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+            const f16x8 vv = (t & 1) ? kv8_f16(va[t / 2].z, va[t / 2].w) : kv8_f16(va[t / 2].x, va[t / 2].y);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                if (PL == 2) o[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, plo[mt], o[mt][t], 0, 0, 0);
+                o[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, ph[mt], o[mt][t], 0, 0, 0);
+            }
+        }
+        if constexpr (more.value) { __builtin_amdgcn_sched_barrier(0); fetch_v(next); }
+    };
+    if (v < v_end) {
+        for (; v + KV8_WAVES < v_end; v += KV8_WAVES) block(std::true_type{});
+        block(std::false_type{});
     }
 
     // ---- the waves of a workgroup, in wave order ----
@@ -413,43 +476,62 @@ __global__ __launch_bounds__(64 * KV8_WAVES) void kv8_attention_kernel(const T *
     }
 }
 
-// Joins the splits of a pair, in split order.
+// Joins the splits of a pair.  64 units (four values of a row) a workgroup, KV8_JOIN threads each: a thread takes every KV8_JOIN-th split,
+// then they meet in LDS in order.
+#define KV8_JOIN 4
 template <typename T>
-__global__ __launch_bounds__(256) void kv8_merge_kernel(const float *__restrict__ part, Kv8Plan pl, int hd, int slots_total, T *__restrict__ out,
-                                                        int64_t ldo, int vec)
+__global__ __launch_bounds__(64 * KV8_JOIN) void kv8_merge_kernel(const float *__restrict__ part, Kv8Plan pl, int hd, int slots_total, T *__restrict__ out,
+                                                                  int64_t ldo, int vec)
 {
+    __shared__ float red[KV8_JOIN][3][64];
+    __shared__ f32x4 acc[KV8_JOIN][64];
     Kv8Part pt;
     if (!kv8_part(pl, (int)blockIdx.y, true, pt) || pt.splits < 2) return;
     const int head = blockIdx.x, b = pt.pair / pl.qgroups, r0 = (pt.pair - b * pl.qgroups) * pl.rg, rows = pl.L * pl.group;
     const size_t rec = kv8_record(pl.rg, hd);
     const float *src = part + ((size_t)head * slots_total + pt.base) * rec;
-    for (int u = threadIdx.x; u < pl.rg * hd / 4; u += 256) {
-        const int lr = u / (hd / 4), d = u % (hd / 4) * 4, r = r0 + lr;
-        if (r >= rows) continue;
-        const float *e = src + pl.rg * hd + lr;
-        float M = -INFINITY, MO = -INFINITY, den = 0.f;
-        for (int s = 0; s < pt.splits; ++s) { M = fmaxf(M, e[s * rec]); MO = fmaxf(MO, e[s * rec + pl.rg]); }
-        f32x4 a = {0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < pt.splits; ++s) {
+    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+    const int u = (int)blockIdx.z * 64 + x, lr = u / (hd / 4), d = u % (hd / 4) * 4, r = r0 + lr;
+    const bool live = lr < pl.rg && r < rows;
+    const float *e = src + pl.rg * hd + lr;
+    float M = -INFINITY, MO = -INFINITY, den = 0.f;
+    f32x4 a = {0.f, 0.f, 0.f, 0.f};
+    if (live) {
+#pragma unroll 4
+        for (int s = y; s < pt.splits; s += KV8_JOIN) {
             const float ms = e[s * rec], mos = e[s * rec + pl.rg], ls = e[s * rec + 2 * pl.rg];
-            den += ms == -INFINITY ? ls : kv8_exp2(ms - M) * ls;
             const float4 v = *reinterpret_cast<const float4 *>(src + s * rec + lr * hd + d);
-            a += (f32x4){v.x, v.y, v.z, v.w} * (mos == -INFINITY ? 1.f : kv8_exp2(mos - MO));
+            const float Mn = fmaxf(M, ms), MOn = fmaxf(MO, mos);
+            den = (M == -INFINITY ? den : den * kv8_exp2(M - Mn)) + (ms == -INFINITY ? ls : ls * kv8_exp2(ms - Mn));
+            a = a * (MO == -INFINITY ? 1.f : kv8_exp2(MO - MOn)) + (f32x4){v.x, v.y, v.z, v.w} * (mos == -INFINITY ? 1.f : kv8_exp2(mos - MOn));
+            M = Mn; MO = MOn;
         }
-        kv8_out(out + ((size_t)b * pl.L + r / pl.group) * ldo + ((size_t)head * pl.group + r % pl.group) * hd + d, a * (kv8_exp2(MO - KV8_LIFT - M) / den), vec & 2);
     }
+    red[y][0][x] = M; red[y][1][x] = MO; red[y][2][x] = den;
+    acc[y][x] = a;
+    __syncthreads();
+    if (y || !live) return;
+#pragma unroll
+    for (int i = 1; i < KV8_JOIN; ++i) {
+        const float ms = red[i][0][x], mos = red[i][1][x], ls = red[i][2][x];
+        const float Mn = fmaxf(M, ms), MOn = fmaxf(MO, mos);
+        den = (M == -INFINITY ? den : den * kv8_exp2(M - Mn)) + (ms == -INFINITY ? ls : ls * kv8_exp2(ms - Mn));
+        a = a * (MO == -INFINITY ? 1.f : kv8_exp2(MO - MOn)) + acc[i][x] * (mos == -INFINITY ? 1.f : kv8_exp2(mos - MOn));
+        M = Mn; MO = MOn;
+    }
+    kv8_out(out + ((size_t)b * pl.L + r / pl.group) * ldo + ((size_t)head * pl.group + r % pl.group) * hd + d, a * (kv8_exp2(MO - KV8_LIFT - M) / den), vec & 2);
 }
 
 static int kv8_plan(int n_seqs, int L, int n_heads, int n_kv, int hd, int cap, Kv8Plan *pl, int *slots_total)
 {
     if (!kv8_sizes(n_seqs, L, n_kv, hd, cap) || n_heads < n_kv || n_heads % n_kv || n_heads > KV8_MAX_HEADS) return SJD_EINVAL;
     const int64_t rows = (int64_t)L * (n_heads / n_kv);
-    const int rg = rows > 16 ? 32 : 16;
+    const int rg = rows > 16 && hd <= 128 ? 32 : 16;       // (32 rows of heads of 256 do not fit 256 registers)
     const int64_t pairs = n_seqs * ((rows + rg - 1) / rg);
     if (rows > INT32_MAX - 64 || pairs > 65535) return SJD_EINVAL;
     pl->n_seqs = n_seqs; pl->L = L; pl->group = n_heads / n_kv; pl->qgroups = (int)((rows + rg - 1) / rg); pl->rg = rg;
     pl->cap = cap; pl->nblk = (cap + 31) / 32;
-    pl->slots = pairs * n_kv >= 512 ? 0 : std::max(1, 768 / n_kv);
+    pl->slots = pairs * n_kv >= 192 ? 0 : std::max(1, 256 / n_kv);
     *slots_total = (int)pairs + pl->slots;
     return SJD_OK;
 }
@@ -483,8 +565,8 @@ extern "C" int sjd_kv8_attention(int32_t dtype, const void *q, int64_t ldq, cons
     hipStream_t s = (hipStream_t)stream;
     const dim3 grid(n_kv_heads, slots);
 #define GO(HD, MT, T) SJD_LAUNCH((kv8_attention_kernel<HD, MT, T>), grid, dim3(64 * KV8_WAVES), 0, s, (const T *)q, ldq, cache, scales, pl, (T *)out, ldo, vec, (float *)workspace)
-#define GO2(HD) do { if (pl.rg == 16) { if (dtype == 0) GO(HD, 1, float); else GO(HD, 1, bf16_t); } \
-                     else { if (dtype == 0) GO(HD, 2, float); else GO(HD, 2, bf16_t); } } while (0)
+#define GO1(HD, MT) do { if (dtype == 0) GO(HD, MT, float); else GO(HD, MT, bf16_t); } while (0)
+#define GO2(HD) do { if (pl.rg == 16) GO1(HD, 1); else if constexpr (HD <= 128) GO1(HD, 2); } while (0)
     switch (head_dim) {
         case 32: GO2(32); break;
         case 64: GO2(64); break;
@@ -493,12 +575,14 @@ extern "C" int sjd_kv8_attention(int32_t dtype, const void *q, int64_t ldq, cons
         default: GO2(256); break;
     }
 #undef GO2
+#undef GO1
 #undef GO
     HIP_TRY(hipGetLastError());
     if (pl.slots) {
-        const dim3 mgrid(n_kv_heads, pl.n_seqs * pl.qgroups);
-        if (dtype == 0) SJD_LAUNCH((kv8_merge_kernel<float>), mgrid, dim3(256), 0, s, (const float *)workspace, pl, head_dim, slots, (float *)out, ldo, vec);
-        else SJD_LAUNCH((kv8_merge_kernel<bf16_t>), mgrid, dim3(256), 0, s, (const float *)workspace, pl, head_dim, slots, (bf16_t *)out, ldo, vec);
+        const int join = 64 * KV8_JOIN, units = std::min(pl.rg, pl.L * pl.group) * (head_dim / 4);
+        const dim3 mgrid(n_kv_heads, pl.n_seqs * pl.qgroups, (units + 63) / 64);
+        if (dtype == 0) SJD_LAUNCH((kv8_merge_kernel<float>), mgrid, dim3(join), 0, s, (const float *)workspace, pl, head_dim, slots, (float *)out, ldo, vec);
+        else SJD_LAUNCH((kv8_merge_kernel<bf16_t>), mgrid, dim3(join), 0, s, (const float *)workspace, pl, head_dim, slots, (bf16_t *)out, ldo, vec);
         HIP_TRY(hipGetLastError());
     }
     return SJD_OK;
