@@ -7,6 +7,7 @@
 #include "sjd_mx.h"
 
 #include <algorithm>
+#include <type_traits>
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
@@ -43,47 +44,296 @@ __device__ __forceinline__ void mx_store4(bf16_t *p, const f32x4 &v, int n, bool
     else for (int i = 0; i < 4; ++i) if (i < n) p[i] = f32_to_bf16(v[i]);
 }
 
-// A wave owns 16 features x 16 rows for the whole reduction.
-template <int FMT, typename T>
-__global__ __launch_bounds__(256) void mx_product_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
+// acc += W A^T for one step of 128 values
+template <int FMT, bool EXACT> __device__ __forceinline__ f32x4 mx_step(const uint4 &w, uint4 a0, uint4 a1, f32x4 acc, int ws, int as)
+{
+    if (FMT == SJD_MX8 && EXACT) {
+        const uint4 m0 = mx_large4(a0), m1 = mx_large4(a1);
+        acc = mx_mfma<FMT>(w, mx_andn(a0, m0), mx_andn(a1, m1), acc, ws, as);
+        a0 = mx_and(a0, m0); a1 = mx_and(a1, m1);
+    }
+    return mx_mfma<FMT>(w, a0, a1, acc, ws, as);
+}
+
+// Buffer descriptors: scalar offsets, and loads whose vector offset lies behind the end give zeros and cost no memory access (scalar offsets
+// stay inside: the hardware takes them from the size before it compares).
+#define MX_OOB 0x40000000        // behind every buffer here
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_buffer(const uint8_t *p, size_t bytes)
+{
+    // (uniform, and said so: else every load becomes a loop over the wave's descriptors)
+    const uint64_t a = (uint64_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc((void *)((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
+}
+__device__ __forceinline__ uint4 mx_load16(__amdgpu_buffer_rsrc_t r, int v, int s)
+{
+    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(r, v, s, 0);
+    return make_uint4(x[0], x[1], x[2], x[3]);
+}
+
+// ---- few rows -------------------------------------------------------------------------------
+// A workgroup owns TN tiles of features and up to 16 MT rows; its waves take the records of a tile in turn, so K is split eight ways, and their
+// sums meet in LDS in wave order.  A wave has one record of every tile (4 steps of 128 values) and its activations in flight: each
+// step's registers are refilled as soon as its products are issued.
+template <int FMT, int MT, int TN, typename T>
+__global__ __launch_bounds__(512, 2) void mx_rows_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                          const uint8_t *__restrict__ packed, int M, int N, int Kp, int tiles, int groups,
                                                          T *__restrict__ C, int64_t ldc, int vec)
 {
-    const int lane = threadIdx.x & 63, q = lane >> 4, c = lane & 15;
-    const int t = (int)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (t >= tiles) return;
-    const int64_t row = (int64_t)blockIdx.y * 16 + c;
-    const bool live = row < M;
-    const int64_t r = live ? row : 0;                       // (rows behind the last are computed on row 0 and not written)
-    const int steps = Kp / 128;
-    const size_t abytes = FMT == SJD_MX8 ? Kp : Kp / 2;
-    const uint8_t *a = codes + (size_t)r * abytes + 16 * q, *as = scales + (size_t)r * (Kp / 32) + q;
-    const uint8_t *w = packed + (size_t)t * groups * MX_REC;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < steps; ++k) {
-        const uint8_t *rec = w + (size_t)(k >> 2) * MX_REC;
-        const uint4 wv = *reinterpret_cast<const uint4 *>(rec + (k & 3) * 1024 + lane * 16);
-        const int ws = rec[4096 + lane * 4 + (k & 3)];
-        uint4 a0, a1 = make_uint4(0, 0, 0, 0);
-        if (FMT == SJD_MX8) {
-            a0 = *reinterpret_cast<const uint4 *>(a + (size_t)k * 128);
-            a1 = *reinterpret_cast<const uint4 *>(a + (size_t)k * 128 + 64);
-        } else a0 = *reinterpret_cast<const uint4 *>(a + (size_t)k * 64);
-        if (FMT == SJD_MX8 && sizeof(T) == 4) {
-            const uint4 m0 = mx_large4(a0), m1 = mx_large4(a1);
-            acc = mx_mfma<FMT>(wv, mx_andn(a0, m0), mx_andn(a1, m1), acc, ws, as[(size_t)k * 4]);
-            a0 = mx_and(a0, m0); a1 = mx_and(a1, m1);
+    constexpr int WK = 8, F = MT * TN, NA = FMT == SJD_MX8 ? 2 : 1;
+    constexpr bool EXACT = sizeof(T) == 4;
+    __shared__ f32x4 red[WK][F][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
+    const int t0 = (int)blockIdx.x * TN, steps = Kp / 128, arow = FMT == SJD_MX8 ? Kp : Kp / 2, srow = Kp / 32;
+    const int64_t row0 = (int64_t)blockIdx.y * (16 * MT);
+    const int live = (int)min((int64_t)(16 * MT), M - row0);
+    const auto wb = mx_buffer(packed + (size_t)t0 * groups * MX_REC, (size_t)min(TN, tiles - t0) * groups * MX_REC);
+    const auto ab = mx_buffer(codes + (size_t)row0 * arow, (size_t)live * arow), sb = mx_buffer(scales + (size_t)row0 * srow, (size_t)live * srow);
+    int va[MT], vs[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) { va[mt] = (mt * 16 + c) * arow + 16 * q; vs[mt] = (mt * 16 + c) * srow; }
+
+    f32x4 acc[MT][TN];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int t = 0; t < TN; ++t) acc[mt][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    uint4 w[4][TN], a[4][MT][NA];
+    int ws[TN], wn[TN], as[4][MT];
+    const int last = min(TN, tiles - t0) - 1;              // (tiles behind the last read it again, and are not written)
+    auto load_scales = [&](int g) {
+#pragma unroll
+        for (int t = 0; t < TN; ++t) wn[t] = __builtin_amdgcn_raw_buffer_load_b32(wb, lane * 4, (min(t, last) * groups + g) * MX_REC + 4096, 0);
+    };
+    auto load_step = [&](int g, int s) {
+        const bool in = g * 4 + s < steps;                 // (the last record has steps behind K)
+        const int k = in ? g * 4 + s : 0, oob = in ? 0 : MX_OOB;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int i = 0; i < NA; ++i) a[s][mt][i] = mx_load16(ab, va[mt] + oob, k * (64 * NA) + 64 * i);
+            as[s][mt] = __builtin_amdgcn_raw_buffer_load_b32(sb, vs[mt] + oob, k * 4, 0);
         }
-        acc = mx_mfma<FMT>(wv, a0, a1, acc, ws, as[(size_t)k * 4]);
+#pragma unroll
+        for (int t = 0; t < TN; ++t) w[s][t] = mx_load16(wb, lane * 16 + oob, (min(t, last) * groups + g) * MX_REC + s * 1024);
+    };
+    auto step = [&](int s) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const int ax = (int)((uint32_t)as[s][mt] >> (8 * q));
+            uint4 lo[NA], hi[NA];
+            if (FMT == SJD_MX8 && EXACT) {
+#pragma unroll
+                for (int i = 0; i < NA; ++i) {
+                    const uint4 m = mx_large4(a[s][mt][i]);
+                    lo[i] = mx_andn(a[s][mt][i], m); hi[i] = mx_and(a[s][mt][i], m);
+                }
+#pragma unroll
+                for (int t = 0; t < TN; ++t) acc[mt][t] = mx_mfma<FMT>(w[s][t], lo[0], lo[NA - 1], acc[mt][t], ws[t] >> (8 * s), ax);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NA; ++i) hi[i] = a[s][mt][i];
+            }
+#pragma unroll
+            for (int t = 0; t < TN; ++t) acc[mt][t] = mx_mfma<FMT>(w[s][t], hi[0], NA == 2 ? hi[NA - 1] : make_uint4(0, 0, 0, 0), acc[mt][t], ws[t] >> (8 * s), ax);
+        }
+    };
+    int g = wave;
+    if (g < groups) {
+        load_scales(g);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) load_step(g, s);
+        for (; g + WK < groups; g += WK) {
+#pragma unroll
+            for (int t = 0; t < TN; ++t) ws[t] = wn[t];
+            load_scales(g + WK);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                step(s);
+                __builtin_amdgcn_sched_barrier(0);
+                load_step(g + WK, s);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < TN; ++t) ws[t] = wn[t];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) step(s);
     }
-    const int n = t * 16 + 4 * q;
-    if (live && n < N) mx_store4(C + row * ldc + n, acc, N - n, vec);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int t = 0; t < TN; ++t) red[wave][mt * TN + t][lane] = acc[mt][t];
+    __syncthreads();
+    for (int f = wave; f < F; f += WK) {
+        const int mt = f / TN, t = f % TN, n = (t0 + t) * 16 + 4 * q;
+        f32x4 x = red[0][f][lane];
+#pragma unroll
+        for (int i = 1; i < WK; ++i) x += red[i][f][lane];
+        const int64_t row = row0 + mt * 16 + c;
+        if (row < M && n < N) mx_store4(C + row * ldc + n, x, N - n, vec);
+    }
+}
+
+// ---- many rows ------------------------------------------------------------------------------
+// A workgroup makes BM rows x BN features.  Its waves share the activations of a step (BM x 128 codes and their scales) through LDS: requested
+// a step ahead, parked in the other of two buffers when the step's products are done, one barrier a step.  Weights go straight to registers,
+// a step ahead too, in the order in which they are packed.  The 16-byte pieces of a row of LDS change places by the row's number, so that eight
+// lanes that read the same piece of eight rows meet all banks once.
+template <int FMT, int WM, int WN, int MT, int NT, typename T>
+__global__ __launch_bounds__(64 * WM * WN, 2) void mx_tile_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
+                                                                  const uint8_t *__restrict__ packed, int M, int N, int Kp, int tiles, int groups,
+                                                                  int per, T *__restrict__ C, int64_t ldc, int vec, float *__restrict__ part)
+{
+    constexpr int W = WM * WN, BM = WM * MT * 16, NA = FMT == SJD_MX8 ? 2 : 1, ROW = 64 * NA, PC = ROW / 16;
+    constexpr bool EXACT = sizeof(T) == 4;
+    constexpr int LOADS = BM * PC / (64 * W);                  // 16-byte loads to LDS a thread makes a step
+    static_assert(BM * PC % (64 * W) == 0 && LOADS >= 1, "");
+    __shared__ uint4 a_lds[2][BM * PC];
+    __shared__ uint32_t s_lds[2][BM];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
+    const int wm = wave / WN, wn = wave % WN;
+    const int64_t row0 = (int64_t)blockIdx.y * BM;
+    const int t0 = ((int)blockIdx.x * WN + wn) * NT, tb = min(t0, tiles - 1), last = min(NT, tiles - tb) - 1;
+    const int arow = FMT == SJD_MX8 ? Kp : Kp / 2, srow = Kp / 32, steps = Kp / 128;
+    const int k_beg = (int)blockIdx.z * per, k_end = min(steps, k_beg + per);
+    const auto wb = mx_buffer(packed + (size_t)tb * groups * MX_REC, (size_t)(last + 1) * groups * MX_REC);   // (tiles behind the last read it again)
+
+    // what this thread copies: piece p of row r goes to place p ^ f(r); rows behind the last repeat it
+    const int live = (int)min((int64_t)BM, M - row0);
+    const auto ab = mx_buffer(codes + (size_t)row0 * arow, (size_t)live * arow), sb = mx_buffer(scales + (size_t)row0 * srow, (size_t)live * srow);
+    int src[LOADS], dst[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int slot = i * 64 * W + (int)threadIdx.x, r = slot / PC, p = slot % PC;
+        src[i] = r * arow + p * 16;                            // (rows behind the last: zeros)
+        dst[i] = r * PC + (PC == 8 ? p ^ (r & 7) : p ^ ((r >> 1) & 3));
+    }
+    const int srow0 = (int)threadIdx.x % BM;                   // (threads too many for the rows copy some twice)
+    uint4 ga[LOADS];
+    uint32_t gs;
+    auto fetch = [&](int k) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) ga[i] = mx_load16(ab, src[i], k * ROW);
+        gs = __builtin_amdgcn_raw_buffer_load_b32(sb, srow0 * srow, k * 4, 0);
+    };
+    auto park = [&](int st) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) a_lds[st][dst[i]] = ga[i];
+        s_lds[st][srow0] = gs;
+    };
+    uint4 w[NT];
+    int ws[NT];
+    auto load_w = [&](int k) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int rec = (min(t, last) * groups + (k >> 2)) * MX_REC;
+            w[t] = mx_load16(wb, lane * 16, rec + (k & 3) * 1024);
+            ws[t] = __builtin_amdgcn_raw_buffer_load_b32(wb, lane * 4, rec + 4096, 0);
+        }
+    };
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[mt][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    auto step = [&](int k, auto more) {
+        const int st = (k - k_beg) & 1;
+        uint4 wc[NT];
+        int wsc[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) { wc[t] = w[t]; wsc[t] = (int)((uint32_t)ws[t] >> (8 * (k & 3))); }
+        __syncthreads();                                       // step k is parked, step k - 1 has been read
+        if constexpr (more.value) { load_w(k + 1); fetch(k + 1); __builtin_amdgcn_sched_barrier(0); }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const int r = (wm * MT + mt) * 16 + c;
+            uint4 a[2];
+#pragma unroll
+            for (int i = 0; i < NA; ++i) {
+                const int piece = i * 4 + q;
+                a[i] = a_lds[st][r * PC + (PC == 8 ? piece ^ (c & 7) : piece ^ ((c >> 1) & 3))];
+            }
+            if (NA == 1) a[1] = make_uint4(0, 0, 0, 0);
+            const int as = (int)(s_lds[st][r] >> (8 * q));
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[mt][t] = mx_step<FMT, EXACT>(wc[t], a[0], a[1], acc[mt][t], wsc[t], as);
+        }
+        if constexpr (more.value) { __builtin_amdgcn_sched_barrier(0); park(st ^ 1); }
+    };
+    load_w(k_beg);
+    fetch(k_beg);
+    park(0);
+    for (int k = k_beg; k < k_end - 1; ++k) step(k, std::true_type{});
+    step(k_end - 1, std::false_type{});
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int64_t row = row0 + (wm * MT + mt) * 16 + c;
+        if (row >= M) continue;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int n = (t0 + t) * 16 + 4 * q;
+            if (n >= N) continue;
+            if (gridDim.z > 1) mx_store4(part + ((size_t)blockIdx.z * M + row) * mx_up(N, 4) + n, acc[mt][t], 4, true);
+            else mx_store4(C + row * ldc + n, acc[mt][t], N - n, vec);
+        }
+    }
+}
+
+// adds the K-slices in their order
+template <typename T>
+__global__ __launch_bounds__(256) void mx_join_kernel(const float *__restrict__ part, int slices, int M, int N, T *__restrict__ C, int64_t ldc, int vec)
+{
+    const int Np = mx_up(N, 4);
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, total = (int64_t)M * (Np / 4);
+    if (i >= total) return;
+    const float4 *p = reinterpret_cast<const float4 *>(part) + i;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < slices; ++s) {
+        const float4 v = p[s * total];
+        x += (f32x4){v.x, v.y, v.z, v.w};
+    }
+    const int64_t row = i / (Np / 4);
+    const int n = (int)(i - row * (Np / 4)) * 4;
+    mx_store4(C + row * ldc + n, x, N - n, vec);
+}
+
+// How a product runs: few rows (TN tiles a workgroup), or tiles of 64 x 128, 128 x 128 or 256 x 256 with K cut into slices.
+struct MxPlan { int kind, tn, mt, slices, per; };
+static MxPlan mx_plan(int M, int N, int K)
+{
+    MxPlan p = {0, 1, 1, 1, 0};
+    const int tiles = (int)(((int64_t)N + 15) / 16), steps = mx_up(K, 128) / 128;
+    if (M <= 32) {
+        p.mt = M <= 16 ? 1 : 2;
+        // the tiles of a workgroup: a CU takes as long as its workgroups' weights (lines from HBM cost about three times those from L2)
+        // and activations together
+        double best = 0;
+        for (int tn : {1, 2, 3, 4, 6}) {
+            if (p.mt == 2 && tn > 4) continue;
+            const double rounds = std::max(1.0, (double)(((tiles + tn - 1) / tn + 255) / 256));
+            const double cost = rounds * (tn * 16 * 0.53 * 3 + M);
+            if (best == 0 || cost < best) { best = cost; p.tn = tn; }
+        }
+        return p;
+    }
+    p.kind = M <= 64 ? 1 : M <= 512 ? 2 : 3;
+    const int bm = p.kind == 1 ? 64 : p.kind == 2 ? 128 : 256, bn = p.kind == 3 ? 256 : 128;
+    const int64_t wgs = (((int64_t)M + bm - 1) / bm) * (((int64_t)N + bn - 1) / bn);
+    int slices = (int)std::min<int64_t>(8, 256 / std::max<int64_t>(wgs, 1));
+    slices = std::max(1, std::min(slices, steps / 8));
+    p.per = (steps + slices - 1) / slices;
+    p.slices = (steps + p.per - 1) / p.per;
+    return p;
 }
 
 extern "C" int sjd_mx_product_workspace(int32_t M, int32_t N, int32_t K, size_t *bytes)
 {
     if (!bytes || M < 1 || N < 1 || K < 1 || K > SJD_MX_MAX_K) return SJD_EINVAL;
-    *bytes = 0;
+    const MxPlan p = mx_plan(M, N, K);
+    *bytes = p.slices > 1 ? (size_t)p.slices * M * mx_up(N, 4) * sizeof(float) : 0;
     return SJD_OK;
 }
 
@@ -97,14 +347,34 @@ extern "C" int sjd_mx_product(int32_t format, const uint8_t *codes, const uint8_
     SJD_TRY(sjd_mx_product_workspace(M, N, K, &need));
     if (need && (!workspace || workspace_bytes < need || !mx_aligned(workspace))) return SJD_EINVAL;
     const int Kp = mx_up(K, 128), tiles = (int)(((int64_t)N + 15) / 16), groups = mx_groups(K);
-    if (((int64_t)M + 15) / 16 > 65535) return SJD_EINVAL;
+    const MxPlan p = mx_plan(M, N, K);
+    if (((int64_t)M + 255) / 256 > 65535) return SJD_EINVAL;
     const int vec = (uintptr_t)C % (dtype ? 8 : 16) == 0 && ldc % 4 == 0;
-    const dim3 grid((tiles + 3) / 4, (M + 15) / 16);
     hipStream_t s = (hipStream_t)stream;
-#define GO(F, T) SJD_LAUNCH((mx_product_kernel<F, T>), grid, dim3(256), 0, s, codes, scales, packed, M, N, Kp, tiles, groups, (T *)C, ldc, vec)
+    float *part = (float *)workspace;
+#define ROWS(F, MT, TN, T) SJD_LAUNCH((mx_rows_kernel<F, MT, TN, T>), dim3((tiles + TN - 1) / TN, (M + 16 * MT - 1) / (16 * MT)), dim3(512), 0, s, codes, scales, packed, M, N, Kp, tiles, groups, (T *)C, ldc, vec)
+#define TILE(F, WM, WN, MT, NT, T) SJD_LAUNCH((mx_tile_kernel<F, WM, WN, MT, NT, T>), dim3((tiles + WN * NT - 1) / (WN * NT), (M + WM * MT * 16 - 1) / (WM * MT * 16), p.slices), \
+                                              dim3(64 * WM * WN), 0, s, codes, scales, packed, M, N, Kp, tiles, groups, p.per, (T *)C, ldc, vec, part)
+#define GO(F, T) do { \
+        if (p.kind == 1) TILE(F, 1, 4, 4, 2, T); \
+        else if (p.kind == 2) TILE(F, 1, 4, 8, 2, T); \
+        else if (p.kind == 3) TILE(F, 2, 4, 8, 4, T); \
+        else if (p.mt == 1) { \
+            if (p.tn == 1) ROWS(F, 1, 1, T); else if (p.tn == 2) ROWS(F, 1, 2, T); else if (p.tn == 3) ROWS(F, 1, 3, T); else if (p.tn == 4) ROWS(F, 1, 4, T); else ROWS(F, 1, 6, T); \
+        } else { \
+            if (p.tn == 1) ROWS(F, 2, 1, T); else if (p.tn == 2) ROWS(F, 2, 2, T); else if (p.tn == 3) ROWS(F, 2, 3, T); else ROWS(F, 2, 4, T); \
+        } } while (0)
     if (format == SJD_MX8) { if (dtype == 0) GO(SJD_MX8, float); else GO(SJD_MX8, bf16_t); }
     else { if (dtype == 0) GO(SJD_MX4, float); else GO(SJD_MX4, bf16_t); }
 #undef GO
+#undef TILE
+#undef ROWS
     HIP_TRY(hipGetLastError());
+    if (p.slices > 1) {
+        const dim3 grid((unsigned)(((int64_t)M * (mx_up(N, 4) / 4) + 255) / 256));
+        if (dtype == 0) SJD_LAUNCH((mx_join_kernel<float>), grid, dim3(256), 0, s, (const float *)part, p.slices, M, N, (float *)C, ldc, vec);
+        else SJD_LAUNCH((mx_join_kernel<bf16_t>), grid, dim3(256), 0, s, (const float *)part, p.slices, M, N, (bf16_t *)C, ldc, vec);
+        HIP_TRY(hipGetLastError());
+    }
     return SJD_OK;
 }
