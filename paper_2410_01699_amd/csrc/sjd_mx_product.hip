@@ -7,6 +7,7 @@
 #include "sjd_mx.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
@@ -99,12 +100,16 @@ __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const uint8_t *__restri
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int t = 0; t < TN; ++t) acc[mt][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    uint4 w[4][TN], a[4][MT][NA];
-    int ws[TN], wn[TN], as[4][MT];
+    uint4 w[4][TN], a[4][MT][NA], as[MT], an[MT];
+    int ws[TN], wn[TN];
     const int last = min(TN, tiles - t0) - 1;              // (tiles behind the last read it again, and are not written)
     auto load_scales = [&](int g) {
 #pragma unroll
         for (int t = 0; t < TN; ++t) wn[t] = __builtin_amdgcn_raw_buffer_load_b32(wb, lane * 4, (min(t, last) * groups + g) * MX_REC + 4096, 0);
+        // (a row's scales of four steps; a step at a time they would be as many lines as the activations themselves.  Behind K they are
+        // another row's, and meet weights of zero)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) an[mt] = mx_load16(sb, vs[mt], g * 16);
     };
     auto load_step = [&](int g, int s) {
         const bool in = g * 4 + s < steps;                 // (the last record has steps behind K)
@@ -113,7 +118,6 @@ __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const uint8_t *__restri
         for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
             for (int i = 0; i < NA; ++i) a[s][mt][i] = mx_load16(ab, va[mt] + oob, k * (64 * NA) + 64 * i);
-            as[s][mt] = __builtin_amdgcn_raw_buffer_load_b32(sb, vs[mt] + oob, k * 4, 0);
         }
 #pragma unroll
         for (int t = 0; t < TN; ++t) w[s][t] = mx_load16(wb, lane * 16 + oob, (min(t, last) * groups + g) * MX_REC + s * 1024);
@@ -121,7 +125,7 @@ __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const uint8_t *__restri
     auto step = [&](int s) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            const int ax = (int)((uint32_t)as[s][mt] >> (8 * q));
+            const int ax = (int)((s == 0 ? as[mt].x : s == 1 ? as[mt].y : s == 2 ? as[mt].z : as[mt].w) >> (8 * q));
             uint4 lo[NA], hi[NA];
             if (FMT == SJD_MX8 && EXACT) {
 #pragma unroll
@@ -147,6 +151,8 @@ __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const uint8_t *__restri
         for (; g + WK < groups; g += WK) {
 #pragma unroll
             for (int t = 0; t < TN; ++t) ws[t] = wn[t];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) as[mt] = an[mt];
             load_scales(g + WK);
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
@@ -158,6 +164,8 @@ __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const uint8_t *__restri
         }
 #pragma unroll
         for (int t = 0; t < TN; ++t) ws[t] = wn[t];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) as[mt] = an[mt];
 #pragma unroll
         for (int s = 0; s < 4; ++s) step(s);
     }
@@ -178,10 +186,10 @@ __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const uint8_t *__restri
 
 // ---- many rows ------------------------------------------------------------------------------
 // A workgroup makes BM rows x BN features.  Its waves share the activations of a step (BM x 128 codes and their scales) through LDS: requested
-// a step ahead, parked in the other of two buffers when the step's products are done, one barrier a step.  Weights go straight to registers,
-// a step ahead too, in the order in which they are packed.  The 16-byte pieces of a row of LDS change places by the row's number, so that eight
+// AHEAD steps ahead, parked in the other of two buffers when a step's products are done, one barrier a step.  Weights go straight to registers,
+// as far ahead, in the order in which they are packed.  The 16-byte pieces of a row of LDS change places by the row's number, so that eight
 // lanes that read the same piece of eight rows meet all banks once.
-template <int FMT, int WM, int WN, int MT, int NT, typename T>
+template <int FMT, int WM, int WN, int MT, int NT, int AHEAD, typename T>
 __global__ __launch_bounds__(64 * WM * WN, 2) void mx_tile_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                                   const uint8_t *__restrict__ packed, int M, int N, int Kp, int tiles, int groups,
                                                                   int per, T *__restrict__ C, int64_t ldc, int vec, float *__restrict__ part)
@@ -190,83 +198,101 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_tile_kernel(const uint8_t 
     constexpr bool EXACT = sizeof(T) == 4;
     constexpr int LOADS = BM * PC / (64 * W);                  // 16-byte loads to LDS a thread makes a step
     static_assert(BM * PC % (64 * W) == 0 && LOADS >= 1, "");
-    __shared__ uint4 a_lds[2][BM * PC];
-    __shared__ uint32_t s_lds[2][BM];
+    __shared__ uint4 a_lds[2][BM * PC], s_lds[2][BM];          // s_lds: a row's scales of four steps
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
     const int wm = wave / WN, wn = wave % WN;
-    const int64_t row0 = (int64_t)blockIdx.y * BM;
-    const int t0 = ((int)blockIdx.x * WN + wn) * NT, tb = min(t0, tiles - 1), last = min(NT, tiles - tb) - 1;
+    // Workgroups go to the eight XCDs in turn.  An XCD gets neighbouring tasks, rows first: the workgroups that read the same weights, and
+    // as many as it runs at a time read few more activations than one of them, from its own L2.
+    const int mb = (int)(((int64_t)M + BM - 1) / BM), all = (int)gridDim.x, each = all / 8, more = all % 8, x = (int)blockIdx.x % 8;
+    const int task = x * each + min(x, more) + (int)blockIdx.x / 8;
+    const int64_t row0 = (int64_t)(task % mb) * BM;
+    const int t0 = (task / mb * WN + wn) * NT, tb = min(t0, tiles - 1), last = min(NT, tiles - tb) - 1;
     const int arow = FMT == SJD_MX8 ? Kp : Kp / 2, srow = Kp / 32, steps = Kp / 128;
-    const int k_beg = (int)blockIdx.z * per, k_end = min(steps, k_beg + per);
+    const int k_beg = (int)blockIdx.z * per, k_end = min(steps, k_beg + per);          // (per is a multiple of 4)
     const auto wb = mx_buffer(packed + (size_t)tb * groups * MX_REC, (size_t)(last + 1) * groups * MX_REC);   // (tiles behind the last read it again)
-
-    // what this thread copies: piece p of row r goes to place p ^ f(r); rows behind the last repeat it
     const int live = (int)min((int64_t)BM, M - row0);
     const auto ab = mx_buffer(codes + (size_t)row0 * arow, (size_t)live * arow), sb = mx_buffer(scales + (size_t)row0 * srow, (size_t)live * srow);
-    int src[LOADS], dst[LOADS];
+
+    // what this thread copies: piece p of row r goes to place p ^ f(r)
+    int src[LOADS];
+    constexpr int RS = 64 * W / PC;                            // rows between a thread's pieces, a multiple of 8
+    const int r0 = (int)threadIdx.x / PC, pc = (int)threadIdx.x % PC, dst = r0 * PC + (PC == 8 ? pc ^ (r0 & 7) : pc ^ ((r0 >> 1) & 3));
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-        const int slot = i * 64 * W + (int)threadIdx.x, r = slot / PC, p = slot % PC;
-        src[i] = r * arow + p * 16;                            // (rows behind the last: zeros)
-        dst[i] = r * PC + (PC == 8 ? p ^ (r & 7) : p ^ ((r >> 1) & 3));
-    }
+    for (int i = 0; i < LOADS; ++i) src[i] = (r0 + i * RS) * arow + pc * 16;           // (rows behind the last: zeros)
     const int srow0 = (int)threadIdx.x % BM;                   // (threads too many for the rows copy some twice)
-    uint4 ga[LOADS];
-    uint32_t gs;
-    auto fetch = [&](int k) {
+    uint4 ga[AHEAD][LOADS], w[AHEAD][NT], gs;
+    int ws[NT], wn4[NT];
+    auto fetch = [&](int k, int set) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) ga[i] = mx_load16(ab, src[i], k * ROW);
-        gs = __builtin_amdgcn_raw_buffer_load_b32(sb, srow0 * srow, k * 4, 0);
+        for (int t = 0; t < NT; ++t) w[set][t] = mx_load16(wb, lane * 16, (min(t, last) * groups + (k >> 2)) * MX_REC + (k & 3) * 1024);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) ga[set][i] = mx_load16(ab, src[i], k * ROW);
     };
-    auto park = [&](int st) {
+    auto fetch_scales = [&](int k) {                           // of the four steps from k on
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) a_lds[st][dst[i]] = ga[i];
-        s_lds[st][srow0] = gs;
+        for (int t = 0; t < NT; ++t) wn4[t] = __builtin_amdgcn_raw_buffer_load_b32(wb, lane * 4, (min(t, last) * groups + (k >> 2)) * MX_REC + 4096, 0);
+        gs = mx_load16(sb, srow0 * srow, k * 4);
     };
-    uint4 w[NT];
-    int ws[NT];
-    auto load_w = [&](int k) {
+    auto park = [&](int st, int set) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int rec = (min(t, last) * groups + (k >> 2)) * MX_REC;
-            w[t] = mx_load16(wb, lane * 16, rec + (k & 3) * 1024);
-            ws[t] = __builtin_amdgcn_raw_buffer_load_b32(wb, lane * 4, rec + 4096, 0);
-        }
+        for (int i = 0; i < LOADS; ++i) a_lds[st][dst + i * RS * PC] = ga[set][i];
     };
     f32x4 acc[MT][NT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[mt][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    auto step = [&](int k, auto more) {
-        const int st = (k - k_beg) & 1;
+    // where this lane reads: row c of the wave's first tile, its one or two pieces; the other tiles lie 16 rows on
+    const int at = (wm * MT * 16 + c) * PC, p0 = at + (PC == 8 ? q ^ (c & 7) : q ^ ((c >> 1) & 3)), p1 = at + (PC == 8 ? (4 + q) ^ (c & 7) : 0);
+    // Step k = 4 g + s, whose set of registers is s % AHEAD; step k + AHEAD is fetched into it.  LDS reads run two row tiles ahead of the
+    // products (left alone the compiler takes one register pair and waits for every read).
+    auto step = [&](int k, auto s_) {
+        constexpr int s = s_.value, set = s % AHEAD, nx = (s + 1) % AHEAD, st = s & 1;
         uint4 wc[NT];
-        int wsc[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) { wc[t] = w[t]; wsc[t] = (int)((uint32_t)ws[t] >> (8 * (k & 3))); }
+        for (int t = 0; t < NT; ++t) { wc[t] = w[set][t]; if (s == 0) ws[t] = wn4[t]; }
         __syncthreads();                                       // step k is parked, step k - 1 has been read
-        if constexpr (more.value) { load_w(k + 1); fetch(k + 1); __builtin_amdgcn_sched_barrier(0); }
+        if (s == 0) fetch_scales(min(k + 4, (k_end - 1) & ~3));
+        fetch(min(k + AHEAD, k_end - 1), set);                 // (behind the end the last step again: no branch around loads)
+        __builtin_amdgcn_sched_barrier(0);
+        const uint4 *la = a_lds[st];
+        const uint8_t *ls = reinterpret_cast<const uint8_t *>(s_lds[(k >> 2) & 1]) + (wm * MT * 16 + c) * 16 + s * 4 + q;
+        uint4 ring[2][NA];
+        int as[2];
+        auto read = [&](int mt) {
+            as[mt & 1] = ls[mt * 256];
+            ring[mt & 1][0] = la[p0 + mt * 16 * PC];
+            if (NA == 2) ring[mt & 1][NA - 1] = la[p1 + mt * 16 * PC];
+        };
+        read(0);
+        if (MT > 1) read(1);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            const int r = (wm * MT + mt) * 16 + c;
-            uint4 a[2];
+            __builtin_amdgcn_sched_barrier(0);
+            const uint4 a0 = ring[mt & 1][0], a1 = NA == 2 ? ring[mt & 1][NA - 1] : make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < NA; ++i) {
-                const int piece = i * 4 + q;
-                a[i] = a_lds[st][r * PC + (PC == 8 ? piece ^ (c & 7) : piece ^ ((c >> 1) & 3))];
-            }
-            if (NA == 1) a[1] = make_uint4(0, 0, 0, 0);
-            const int as = (int)(s_lds[st][r] >> (8 * q));
-#pragma unroll
-            for (int t = 0; t < NT; ++t) acc[mt][t] = mx_step<FMT, EXACT>(wc[t], a[0], a[1], acc[mt][t], wsc[t], as);
+            for (int t = 0; t < NT; ++t) acc[mt][t] = mx_step<FMT, EXACT>(wc[t], a0, a1, acc[mt][t], (int)((uint32_t)ws[t] >> (8 * s)), as[mt & 1]);
+            if (mt + 2 < MT) { __builtin_amdgcn_sched_barrier(0); read(mt + 2); }
         }
-        if constexpr (more.value) { __builtin_amdgcn_sched_barrier(0); park(st ^ 1); }
+        __builtin_amdgcn_sched_barrier(0);
+        park(st ^ 1, nx);
+        if (s == 0) s_lds[((k >> 2) & 1) ^ 1][srow0] = gs;      // (last read in the group before this one)
     };
-    load_w(k_beg);
-    fetch(k_beg);
-    park(0);
-    for (int k = k_beg; k < k_end - 1; ++k) step(k, std::true_type{});
-    step(k_end - 1, std::false_type{});
+    fetch_scales(k_beg);
+    fetch(k_beg, 0);
+    if (AHEAD == 2) fetch(min(k_beg + 1, k_end - 1), AHEAD - 1);
+    park(0, 0);
+    s_lds[(k_beg >> 2) & 1][srow0] = gs;
+    int k = k_beg;
+    for (; k + 4 <= k_end; k += 4) {
+        step(k, std::integral_constant<int, 0>());
+        step(k + 1, std::integral_constant<int, 1>());
+        step(k + 2, std::integral_constant<int, 2>());
+        step(k + 3, std::integral_constant<int, 3>());
+    }
+    if (k < k_end) step(k, std::integral_constant<int, 0>());
+    if (k + 1 < k_end) step(k + 1, std::integral_constant<int, 1>());
+    if (k + 2 < k_end) step(k + 2, std::integral_constant<int, 2>());
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         const int64_t row = row0 + (wm * MT + mt) * 16 + c;
@@ -300,33 +326,53 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const float *__restrict__ 
     mx_store4(C + row * ldc + n, x, N - n, vec);
 }
 
-// How a product runs: few rows (TN tiles a workgroup), or tiles of 64 x 128, 128 x 128 or 256 x 256 with K cut into slices.
-struct MxPlan { int kind, tn, mt, slices, per; };
+// ---- which kernel ---------------------------------------------------------------------------
+// Whichever is estimated to be done first.  A launch takes as long as its weights from memory or as the CU with most workgroups: so many
+// steps (records) times what one costs, measured with K = 4096 and cold weights in us, bf16 results, activations in 8 bits:
+//  - tiles, a step of a workgroup alone on its CU and of one among several (below);
+//  - few rows, 0.6 + (records / 8) (1.5 + 0.6 TN) for 16 rows, (3.4 + 0.6 TN) for 32; several workgroups of
+//    16 rows on a CU take a seventh less.
+// Slices of K add their sums' way through memory and a launch.  us, measured, the kernel chosen and the next best ones:
+//   16 rows    22016 x 4096   rows 6 tiles 11.1   3 tiles 11.7, 1 tile 17.0           (weights alone 7.5)
+//   64         4096 x 4096    rows 2 tiles 7.7    rows 4 tiles 9.0, 64 x 64 in 4 slices 10.0
+//   64         22016 x 4096   64 x 128 18.5       64 x 64 20.2, rows 4 tiles 26.9
+//   128        22016 x 4096   64 x 192 21.3       128 x 128 25.0, 64 x 128 26.1
+//   128        4096 x 11008   64 x 128 in 4 slices 17.0   rows 4 tiles 18.5, in 2 slices 23.0
+//   512        4096 x 4096    64 x 128 16.9       128 x 128 23.7, 128 x 192 33.1
+//   2048       22016 x 4096   256 x 256 178       128 x 192 181, 128 x 128 201
+//   2048       4096 x 4096    128 x 256 36.8      128 x 128 39.0, 256 x 256 59.7
+struct MxTile { int bm, bn; double alone, among; };
+static const MxTile mx_tiles[] = {{64, 64, 0.375, 0.26}, {64, 128, 0.45, 0.33}, {64, 192, 0.59, 0.45}, {128, 128, 0.70, 0.57},
+                                  {128, 192, 0.98, 0.78}, {128, 256, 1.07, 1.07}, {256, 256, 1.80, 1.80}};
+struct MxPlan { int kind, tn, mt, slices, per, wgs; };      // kind: -1 few rows, else the tile
 static MxPlan mx_plan(int M, int N, int K)
 {
-    MxPlan p = {0, 1, 1, 1, 0};
-    const int tiles = (int)(((int64_t)N + 15) / 16), steps = mx_up(K, 128) / 128;
-    if (M <= 32) {
-        p.mt = M <= 16 ? 1 : 2;
-        // the tiles of a workgroup: a CU takes as long as its workgroups' weights (lines from HBM cost about three times those from L2)
-        // and activations together
-        double best = 0;
-        for (int tn : {1, 2, 3, 4, 6}) {
-            if (p.mt == 2 && tn > 4) continue;
-            const double rounds = std::max(1.0, (double)(((tiles + tn - 1) / tn + 255) / 256));
-            const double cost = rounds * (tn * 16 * 0.53 * 3 + M);
-            if (best == 0 || cost < best) { best = cost; p.tn = tn; }
-        }
-        return p;
+    const int steps = mx_up(K, 128) / 128, groups = mx_groups(K);
+    const double tiles = (N + 15) / 16, stream = (double)N * K * 0.53 / 5.5e6;          // us from memory
+    MxPlan best = {-1, 1, 1, 1, 0, 0};
+    double cost = 1e30;
+    auto take = [&](double t, const MxPlan &p) { if (t < cost) { cost = t; best = p; } };
+    const int mt = M <= 16 ? 1 : 2;
+    for (int tn : {1, 2, 3, 4, 6}) {
+        if (mt == 2 && tn == 6) continue;
+        const double wgs = std::ceil(tiles / tn) * std::ceil(M / (16.0 * mt)), n = std::ceil(wgs / 256);
+        const double t = n * (0.6 + std::max(groups / 8.0, 0.4) * ((mt == 1 ? 1.5 : 3.4) + 0.6 * tn)) * (n > 1 && mt == 1 ? 0.85 : 1);
+        // (where memory bounds both: the one with less beside it)
+        take(std::max(t, stream) + 0.01 * t, {-1, tn, mt, 1, 0, 0});
     }
-    p.kind = M <= 64 ? 1 : M <= 512 ? 2 : 3;
-    const int bm = p.kind == 1 ? 64 : p.kind == 2 ? 128 : 256, bn = p.kind == 3 ? 256 : 128;
-    const int64_t wgs = (((int64_t)M + bm - 1) / bm) * (((int64_t)N + bn - 1) / bn);
-    int slices = (int)std::min<int64_t>(8, 256 / std::max<int64_t>(wgs, 1));
-    slices = std::max(1, std::min(slices, steps / 8));
-    p.per = (steps + slices - 1) / slices;
-    p.slices = (steps + p.per - 1) / p.per;
-    return p;
+    if (M > 32)
+        for (int k = 0; k < 7; ++k) {
+            const MxTile &x = mx_tiles[k];
+            const int64_t wgs = (int64_t)((M + (int64_t)x.bm - 1) / x.bm) * ((N + (int64_t)x.bn - 1) / x.bn);
+            if (wgs > INT32_MAX) continue;
+            for (int sl = 1; sl <= 4 && (sl == 1 || steps >= 8 * sl); sl *= 2) {
+                const int per = mx_up((steps + sl - 1) / sl, 4), slices = (steps + per - 1) / per;
+                const double n = std::ceil((double)wgs * slices / 256), t = per * (n > 1 ? n * x.among : x.alone);
+                const double join = slices > 1 ? 2.5 + (double)M * N * 4 * (slices + 1) / 5e6 : 0;
+                take(std::max(t, stream) + 0.01 * t + join, {k, 0, 0, slices, per, (int)wgs});
+            }
+        }
+    return best;
 }
 
 extern "C" int sjd_mx_product_workspace(int32_t M, int32_t N, int32_t K, size_t *bytes)
@@ -348,17 +394,21 @@ extern "C" int sjd_mx_product(int32_t format, const uint8_t *codes, const uint8_
     if (need && (!workspace || workspace_bytes < need || !mx_aligned(workspace))) return SJD_EINVAL;
     const int Kp = mx_up(K, 128), tiles = (int)(((int64_t)N + 15) / 16), groups = mx_groups(K);
     const MxPlan p = mx_plan(M, N, K);
-    if (((int64_t)M + 255) / 256 > 65535) return SJD_EINVAL;
+    if (p.kind < 0 && ((int64_t)M + 16 * p.mt - 1) / (16 * p.mt) > 65535) return SJD_EINVAL;
     const int vec = (uintptr_t)C % (dtype ? 8 : 16) == 0 && ldc % 4 == 0;
     hipStream_t s = (hipStream_t)stream;
     float *part = (float *)workspace;
 #define ROWS(F, MT, TN, T) SJD_LAUNCH((mx_rows_kernel<F, MT, TN, T>), dim3((tiles + TN - 1) / TN, (M + 16 * MT - 1) / (16 * MT)), dim3(512), 0, s, codes, scales, packed, M, N, Kp, tiles, groups, (T *)C, ldc, vec)
-#define TILE(F, WM, WN, MT, NT, T) SJD_LAUNCH((mx_tile_kernel<F, WM, WN, MT, NT, T>), dim3((tiles + WN * NT - 1) / (WN * NT), (M + WM * MT * 16 - 1) / (WM * MT * 16), p.slices), \
-                                              dim3(64 * WM * WN), 0, s, codes, scales, packed, M, N, Kp, tiles, groups, p.per, (T *)C, ldc, vec, part)
+#define TILE(F, WM, WN, MT, NT, A, T) SJD_LAUNCH((mx_tile_kernel<F, WM, WN, MT, NT, A, T>), dim3((unsigned)p.wgs, 1, p.slices), \
+                                                 dim3(64 * WM * WN), 0, s, codes, scales, packed, M, N, Kp, tiles, groups, p.per, (T *)C, ldc, vec, part)
 #define GO(F, T) do { \
-        if (p.kind == 1) TILE(F, 1, 4, 4, 2, T); \
-        else if (p.kind == 2) TILE(F, 1, 4, 8, 2, T); \
-        else if (p.kind == 3) TILE(F, 2, 4, 8, 4, T); \
+        if (p.kind == 0) TILE(F, 1, 4, 4, 1, 2, T); \
+        else if (p.kind == 1) TILE(F, 1, 4, 4, 2, 2, T); \
+        else if (p.kind == 2) TILE(F, 1, 4, 4, 3, 2, T); \
+        else if (p.kind == 3) TILE(F, 1, 4, 8, 2, 2, T); \
+        else if (p.kind == 4) TILE(F, 1, 4, 8, 3, 1, T); \
+        else if (p.kind == 5) TILE(F, 1, 8, 8, 2, 1, T); \
+        else if (p.kind == 6) TILE(F, 2, 4, 8, 4, 1, T); \
         else if (p.mt == 1) { \
             if (p.tn == 1) ROWS(F, 1, 1, T); else if (p.tn == 2) ROWS(F, 1, 2, T); else if (p.tn == 3) ROWS(F, 1, 3, T); else if (p.tn == 4) ROWS(F, 1, 4, T); else ROWS(F, 1, 6, T); \
         } else { \
