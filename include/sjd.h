@@ -373,7 +373,7 @@ int sjd_mx_product(int32_t format, const uint8_t *codes, const uint8_t *scales, 
                    int32_t K, int32_t dtype, void *C, int64_t ldc, void *workspace, size_t workspace_bytes, void *stream);
 
 /* A cache in 8 bits of n_seqs sequences, `cap` positions each: cache dev [n_seqs][n_kv_heads][ceil(cap / 32)][64 * head_dim],
- * scales dev [n_seqs][n_kv_heads][ceil(cap / 32)][2] (keys, values).  head_dim: a multiple of 32, at most 256.  A block's record
+ * scales dev [n_seqs][n_kv_heads][ceil(cap / 32)][2] (keys, values).  head_dim: 32, 64, 96, 128 or 256.  A block's record
  * holds its keys, then its values, as the lanes of the attention read them:
  *   K[p][d] at 1024 (o / 2) + 16 l + 8 (o % 2) + d % 8, o = (p / 16)(head_dim / 32) + d / 32, l = 16 (d % 32 / 8) + p % 16
  *   V[p][d] at 32 head_dim + 1024 (o / 2) + 16 l + 8 (o % 2) + 4 (p / 16) + p % 4, o = d / 16, l = 16 (p % 16 / 4) + d % 16

@@ -121,15 +121,21 @@ extern "C" int sjd_kv8_append(int32_t dtype, const void *k, const void *v, int64
 
 // ---- attention ------------------------------------------------------------------------------
 #define KV8_WAVES 8
+#define KV8_ROWS 16
+// Where every walk has up to this many blocks none is split, four blocks a wave, and nothing is joined.  Cut and joined against whole: 9.6 us
+// against 6.6 (300 positions, one query, 32 heads), 10.1 against 8.4 (583, 16 queries); longer walks gain from the cut.
+#define KV8_SHORT 32
 #define KV8_LIFT 14      // probabilities times 2^14 in fp16: 22 bits of hi + lo hold from 2^-27 of the largest on
 
 // The queries of one sequence that read one cache head, L * (heads per cache head) rows with a query's heads next to each other, are cut
-// into groups of 16 or 32 rows.  A (sequence, group) pair walks the blocks that any of its queries sees, the sinks' first.  Where the
-// pairs are too few for the chip their walks are cut into splits, all of about the same number of blocks: lengths live on the device,
-// so the kernels work the cut out themselves, every workgroup the same.
+// into groups of 16 rows.  A (sequence, group) pair walks the blocks that any of its queries sees, the sinks' first.  Where the pairs are too
+// few for the chip their walks are cut into splits, all of about the same number of blocks: lengths live on the device, so the kernels work
+// the cut out themselves, every workgroup the same.
+// What more rows a workgroup gain: two tiles of rows per wave 40.5 us against 42.8 at 32 queries x 4 heads a cache head, 16 k positions, but 29
+// against 22 at 128 queries of one head, 4 k positions (half the workgroups); four to eight tiles over codes made fp16 once in LDS, 50 to 58.
 struct Kv8Plan {
     const int32_t *len;
-    int32_t n_seqs, L, group, qgroups, rg;     // heads per cache head; row groups of `rg` rows per sequence
+    int32_t n_seqs, L, group, qgroups;     // heads per cache head; row groups of KV8_ROWS rows per sequence
     int32_t window, sinks, cap, nblk;
     int32_t slots;                             // splits to aim for per cache head; 0: one per pair, none cut
 };
@@ -137,10 +143,10 @@ struct Kv8Span { int32_t i0, i1, n, first, front, count; };    // queries, cache
 __device__ __forceinline__ Kv8Span kv8_span(const Kv8Plan &pl, int pair)
 {
     Kv8Span s;
-    const int b = pair / pl.qgroups, r0 = (pair - b * pl.qgroups) * pl.rg;
+    const int b = pair / pl.qgroups, r0 = (pair - b * pl.qgroups) * KV8_ROWS;
     s.n = pl.len[b];
     s.i0 = r0 / pl.group;
-    s.i1 = min(r0 + pl.rg - 1, pl.L * pl.group - 1) / pl.group;
+    s.i1 = min(r0 + KV8_ROWS - 1, pl.L * pl.group - 1) / pl.group;
     s.first = s.front = s.count = 0;
     if (s.n < 0 || s.n > pl.cap - pl.L) return s;
     const int last = s.n + s.i1;
@@ -160,12 +166,15 @@ __device__ __forceinline__ bool kv8_part(const Kv8Plan &pl, int want, bool by_pa
     const int pairs = pl.n_seqs * pl.qgroups, lane = threadIdx.x & 63;
     const int c0 = lane < pairs ? kv8_span(pl, lane).count : 0;
     float total = 0.f;
+    uint64_t cut = 0;                                                          // any walk long enough
     for (int p0 = 0; p0 < pairs; p0 += 64) {
-        float c = (float)(p0 == 0 ? c0 : p0 + lane < pairs ? kv8_span(pl, p0 + lane).count : 0);
+        const int n = p0 == 0 ? c0 : p0 + lane < pairs ? kv8_span(pl, p0 + lane).count : 0;
+        float c = (float)n;
+        cut |= __ballot(n > KV8_SHORT);
         for (int o = 1; o < min(pairs, 64); o <<= 1) c += __shfl_xor(c, o);
         total += __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(c)));
     }
-    part.per = max(KV8_WAVES, (int)ceilf(total / (float)pl.slots));
+    part.per = cut ? max(KV8_WAVES, (int)ceilf(total / (float)pl.slots)) : KV8_SHORT;
     int base = 0;
     for (int p0 = 0; p0 < pairs; p0 += 64) {
         const int c = p0 == 0 ? c0 : p0 + lane < pairs ? kv8_span(pl, p0 + lane).count : 0;
@@ -204,13 +213,10 @@ __device__ __forceinline__ float kv8_across(float x)
     return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 __device__ __forceinline__ float kv8_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ void kv8_put(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
 
-// record of a split: O[rg][HD] in units of 2^(mo - KV8_LIFT), then m[rg], mo[rg], l[rg]
-__host__ __device__ __forceinline__ size_t kv8_record(int rg, int hd) { return (size_t)rg * (hd + 3); }
+// record of a split: O[KV8_ROWS][HD] in units of 2^(mo - KV8_LIFT), then m, mo and l of the rows; rows behind the last are not written
+__host__ __device__ __forceinline__ size_t kv8_record(int hd) { return (size_t)KV8_ROWS * (hd + 3); }
 
-__device__ __forceinline__ float kv8_load(const float *p) { return *p; }
-__device__ __forceinline__ float kv8_load(const bf16_t *p) { return bf16_to_f32(*p); }
 __device__ __forceinline__ void kv8_out(float *p, const f32x4 &v, bool vec)
 {
     if (vec) *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
@@ -229,13 +235,13 @@ __device__ __forceinline__ void kv8_out(bf16_t *p, const f32x4 &v, bool vec)
 // O has a reference of its own because the blocks' scales differ: with it the largest contribution is always 2^LIFT, whatever the
 // scales are, and fp16 holds what matters beside it.  out = O * 2^(mo - LIFT - m) / l.
 // The two score tiles of a block leave lane (g, c) with row c and the positions 16 h + 4 g + i: the order in which V's operands hold them.
-template <int HD, int MT, typename T>
-__global__ __launch_bounds__(64 * KV8_WAVES, MT == 1 && HD <= 128 ? 4 : 2) void kv8_attention_kernel(const T *__restrict__ q, int64_t ldq, const uint8_t *__restrict__ cache,
+template <int HD, typename T>
+__global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attention_kernel(const T *__restrict__ q, int64_t ldq, const uint8_t *__restrict__ cache,
                                                                           const uint8_t *__restrict__ scales, Kv8Plan pl, T *__restrict__ out,
                                                                           int64_t ldo, int vec, float *__restrict__ part)
 {
-    constexpr int KS = HD / 32, DT = HD / 16, RG = MT * 16, PL = sizeof(T) == 4 ? 2 : 1, CH = DT < 8 ? DT : 8;
-    __shared__ f16x8 q_lds[MT][KS][PL][64];
+    constexpr int KS = HD / 32, DT = HD / 16, RG = KV8_ROWS, PL = sizeof(T) == 4 ? 2 : 1, CH = DT < 8 ? DT : 8;
+    __shared__ f16x8 q_lds[KS][PL][64];
     __shared__ float q_scale[RG];
     __shared__ float m_all[KV8_WAVES][RG], mo_all[KV8_WAVES][RG], l_all[KV8_WAVES][RG];
     __shared__ f32x4 o_slot[KV8_WAVES][CH][64];
@@ -255,32 +261,35 @@ __global__ __launch_bounds__(64 * KV8_WAVES, MT == 1 && HD <= 128 ? 4 : 2) void 
     int sc = 0;
     auto place = [&](int v) { return v < sp.front ? v : sp.first + v - sp.front; };
     auto fetch_k = [&](int blk) {
-        const uint4 *rec = reinterpret_cast<const uint4 *>(cache + (at0 + blk) * (64 * HD)) + lane;
+        const auto rec = mx_buffer(cache + (at0 + blk) * (64 * HD), 64 * HD);      // (a descriptor in scalars: one register of lane offsets)
 #pragma unroll
-        for (int p = 0; p < KS; ++p) ka[p] = rec[p * 64];
+        for (int p = 0; p < KS; ++p) ka[p] = mx_load16(rec, lane * 16, p * 1024);
         sc = *reinterpret_cast<const uint16_t *>(scales + (at0 + blk) * 2);
     };
     auto fetch_v = [&](int blk) {
-        const uint4 *rec = reinterpret_cast<const uint4 *>(cache + (at0 + blk) * (64 * HD)) + lane;
+        const auto rec = mx_buffer(cache + (at0 + blk) * (64 * HD), 64 * HD);
 #pragma unroll
-        for (int p = 0; p < KS; ++p) va[p] = rec[(KS + p) * 64];
+        for (int p = 0; p < KS; ++p) va[p] = mx_load16(rec, lane * 16, (KS + p) * 1024);
     };
     int v = v_beg + wave;
+    // Q by wave 0: lane (g, c) has values 32 ks + 8 g .. of row c.  Requested first: loads return in order.
+    float x[KS][8];
+    if (wave == 0) {
+        const int r = min(r0 + c, rows - 1);
+        const T *src = q + ((size_t)b * pl.L + r / pl.group) * ldq + ((size_t)head * pl.group + r % pl.group) * HD;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) mx_load8<T>(src, ks * 32 + g * 8, HD, vec & 1, x[ks]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     if (v < v_end) { fetch_k(place(v)); fetch_v(place(v)); }
     __builtin_amdgcn_sched_barrier(0);
 
-    // Q of row tile mt by wave mt: lane (g, c) has values 32 ks + 8 g .. of row c
-    for (int mt = wave; mt < MT; mt += KV8_WAVES) {
-        const int r = min(r0 + mt * 16 + c, rows - 1);
-        float x[KS][8];
+    if (wave == 0) {
         uint32_t top = 0;
-        const T *src = q + ((size_t)b * pl.L + r / pl.group) * ldq + ((size_t)head * pl.group + r % pl.group) * HD;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            mx_load8<T>(src, ks * 32 + g * 8, HD, vec & 1, x[ks]);
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = max(top, mx_finite_bits(x[ks][e]));
-        }
         top = max(top, (uint32_t)__shfl_xor((int)top, 16));
         top = max(top, (uint32_t)__shfl_xor((int)top, 32));
         const int up = min(max(127 + 13 - (int)(top >> 23), -126), 127);        // 2^up * the largest is in 2^13 .. 2^14
@@ -294,101 +303,79 @@ __global__ __launch_bounds__(64 * KV8_WAVES, MT == 1 && HD <= 128 ? 4 : 2) void 
                 hi[e] = (_Float16)y;
                 lo[e] = (_Float16)(y - (float)hi[e]);
             }
-            q_lds[mt][ks][0][lane] = hi;
-            if (PL == 2) q_lds[mt][ks][PL - 1][lane] = lo;
+            q_lds[ks][0][lane] = hi;
+            if (PL == 2) q_lds[ks][PL - 1][lane] = lo;
         }
-        if (g == 0) q_scale[mt * 16 + c] = mx_pow2(127 - up) * (1.4426950408889634f / sqrtf((float)HD));
+        if (g == 0) q_scale[c] = mx_pow2(127 - up) * (1.4426950408889634f / sqrtf((float)HD));
     }
     __syncthreads();
 
-    f32x4 o[MT][DT];
-    float m[MT], mo[MT], l[MT], qs[MT];
-    int pos[MT];
+    f32x4 o[DT];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        m[mt] = mo[mt] = -INFINITY; l[mt] = 0.f;
-        qs[mt] = q_scale[mt * 16 + c];
-        pos[mt] = sp.n + min(r0 + mt * 16 + c, rows - 1) / pl.group;
-#pragma unroll
-        for (int t = 0; t < DT; ++t) o[mt][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    }
+    for (int t = 0; t < DT; ++t) o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, mo = -INFINITY, l = 0.f;
+    const float qs = q_scale[c];
+    const int pos = sp.n + min(r0 + c, rows - 1) / pl.group;
     auto block = [&](auto more) {
         const int blk = place(v), k0 = blk * 32, next = more.value ? place(v + KV8_WAVES) : 0;
         const int sb = __builtin_amdgcn_readfirstlane(sc);
         const float ks2 = mx_pow2(sb & 255), ev = (float)((sb >> 8) - 127);
         const bool whole = k0 + 31 <= sp.n + sp.i0 && (!pl.window || k0 > sp.n + sp.i1 - pl.window || k0 + 31 < pl.sinks);
-        f32x4 s[MT][2];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) s[mt][0] = s[mt][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int op = 0; op < 2 * KS; ++op) {
-            const int h = op / KS, ks = op % KS;
             const f16x8 k = (op & 1) ? kv8_f16(ka[op / 2].z, ka[op / 2].w) : kv8_f16(ka[op / 2].x, ka[op / 2].y);
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-                for (int p = PL - 1; p >= 0; --p) s[mt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q_lds[mt][ks][p][lane], s[mt][h], 0, 0, 0);
-            }
+            for (int p = PL - 1; p >= 0; --p) s[op / KS] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q_lds[op % KS][p][lane], s[op / KS], 0, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (more.value) { fetch_k(next); __builtin_amdgcn_sched_barrier(0); }
-        f16x8 ph[MT], plo[MT];
-        uint32_t seen[MT];
-        float turn[MT];                          // what a row's output so far is rescaled by
-        bool turns = false;
+        f16x8 ph, plo;
+        uint32_t seen = 0xFFu;
+        const float cs = qs * ks2;
+        float x[8], bm;
+        if (whole) {
+            bm = s[0][0];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const float cs = qs[mt] * ks2;
-            float x[8], bm;
-            seen[mt] = 0xFFu;
-            if (whole) {
-                bm = s[mt][0][0];
-#pragma unroll
-                for (int e = 1; e < 8; ++e) bm = fmaxf(bm, s[mt][e >> 2][e & 3]);
-                bm *= cs;
-            } else {
-                bm = -INFINITY;
-                seen[mt] = 0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int key = k0 + (e >> 2) * 16 + g * 4 + (e & 3);
-                    const bool see = key <= pos[mt] && (!pl.window || key > pos[mt] - pl.window || key < pl.sinks);
-                    seen[mt] |= see ? 1u << e : 0u;
-                    x[e] = see ? s[mt][e >> 2][e & 3] * cs : -INFINITY;
-                    bm = fmaxf(bm, x[e]);
-                }
-            }
-            bm = kv8_across(bm);
-            const float mn = fmaxf(m[mt], bm), mon = fmaxf(mo[mt], bm + ev);
-            const float so = mn == -INFINITY ? 1.f : kv8_exp2(m[mt] - mn);
-            const float f = mn == -INFINITY ? 0.f : kv8_exp2(fminf(ev - mon + mn + KV8_LIFT, 120.f));
-            turn[mt] = mon == -INFINITY ? 1.f : kv8_exp2(mo[mt] - mon);
-            turns |= turn[mt] != 1.f;
-            if (whole) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = kv8_exp2(fmaf(s[mt][e >> 2][e & 3], cs, -mn));
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = seen[mt] >> e & 1 ? kv8_exp2(x[e] - mn) : 0.f;
-            }
-            float sum = 0.f;
+            for (int e = 1; e < 8; ++e) bm = fmaxf(bm, s[e >> 2][e & 3]);
+            bm *= cs;
+        } else {
+            bm = -INFINITY;
+            seen = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                sum += x[e];
-                float pf = x[e] * f;
-                if (PL == 2) asm("" : "+v"(pf));     // (the product in fp32 for both parts: fused into the conversion to fp16 it rounds otherwise now and then)
-                ph[mt][e] = (_Float16)pf;
-                if (PL == 2) plo[mt][e] = (_Float16)(pf - (float)ph[mt][e]);
+                const int key = k0 + (e >> 2) * 16 + g * 4 + (e & 3);
+                const bool see = (key <= pos) & ((pl.window == 0) | (key > pos - pl.window) | (key < pl.sinks));
+                seen |= see ? 1u << e : 0u;
+                x[e] = see ? s[e >> 2][e & 3] * cs : -INFINITY;
+                bm = fmaxf(bm, x[e]);
             }
-            l[mt] = l[mt] * so + sum;
-            m[mt] = mn; mo[mt] = mon;
         }
-        if (__ballot(turns)) {                   // (rare once a row has met its largest scores)
+        bm = kv8_across(bm);
+        const float mn = fmaxf(m, bm), mon = fmaxf(mo, bm + ev);
+        const float so = mn == -INFINITY ? 1.f : kv8_exp2(m - mn);
+        const float f = mn == -INFINITY ? 0.f : kv8_exp2(fminf(ev - mon + mn + KV8_LIFT, 120.f));
+        const float turn = mon == -INFINITY ? 1.f : kv8_exp2(mo - mon);      // what the output so far is rescaled by
+        if (whole) {
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int e = 0; e < 8; ++e) x[e] = kv8_exp2(fmaf(s[e >> 2][e & 3], cs, -mn));
+        } else {
 #pragma unroll
-                for (int t = 0; t < DT; ++t) o[mt][t] *= turn[mt];
+            for (int e = 0; e < 8; ++e) x[e] = seen >> e & 1 ? kv8_exp2(x[e] - mn) : 0.f;
         }
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            sum += x[e];
+            float pf = x[e] * f;
+            if (PL == 2) asm("" : "+v"(pf));     // (the product in fp32 for both parts: fused into the conversion to fp16 it rounds otherwise now and then)
+            ph[e] = (_Float16)pf;
+            if (PL == 2) plo[e] = (_Float16)(pf - (float)ph[e]);
+        }
+        l = l * so + sum;
+        m = mn; mo = mon;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[t] *= turn;
         if (!whole) {
             // Zero times NaN is NaN: where a mask may hide a NaN code from some row, the codes are taken out, and the rows that see one
             // get it by counting.
@@ -402,16 +389,14 @@ __global__ __launch_bounds__(64 * KV8_WAVES, MT == 1 && HD <= 128 ? 4 : 2) void 
                     const uint32_t n0 = kv8_nan(w0) >> 7, n1 = kv8_nan(w1) >> 7;        // 1 in the byte of a NaN
                     f16x8 ind, vis;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) ind[e] = (_Float16)(float)(((e < 4 ? n0 : n1) >> (8 * (e & 3))) & 1u);
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) vis[e] = (_Float16)(float)(seen[mt] >> e & 1u);
-                        f32x4 hits = {0.f, 0.f, 0.f, 0.f};
-                        hits = __builtin_amdgcn_mfma_f32_16x16x32_f16(ind, vis, hits, 0, 0, 0);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) if (hits[i] != 0.f) o[mt][t][i] = NAN;
+                    for (int e = 0; e < 8; ++e) {
+                        ind[e] = (_Float16)(float)(((e < 4 ? n0 : n1) >> (8 * (e & 3))) & 1u);
+                        vis[e] = (_Float16)(float)(seen >> e & 1u);
                     }
+                    f32x4 hits = {0.f, 0.f, 0.f, 0.f};
+                    hits = __builtin_amdgcn_mfma_f32_16x16x32_f16(ind, vis, hits, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) if (hits[i] != 0.f) o[t][i] = NAN;
                     w0 &= ~(n0 * 0xFFu); w1 &= ~(n1 * 0xFFu);
                 }
             }
@@ -419,11 +404,8 @@ __global__ __launch_bounds__(64 * KV8_WAVES, MT == 1 && HD <= 128 ? 4 : 2) void 
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
             const f16x8 vv = (t & 1) ? kv8_f16(va[t / 2].z, va[t / 2].w) : kv8_f16(va[t / 2].x, va[t / 2].y);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                if (PL == 2) o[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, plo[mt], o[mt][t], 0, 0, 0);
-                o[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, ph[mt], o[mt][t], 0, 0, 0);
-            }
+            if (PL == 2) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, plo, o[t], 0, 0, 0);
+            o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, ph, o[t], 0, 0, 0);
         }
         if constexpr (more.value) { __builtin_amdgcn_sched_barrier(0); fetch_v(next); }
     };
@@ -433,47 +415,38 @@ __global__ __launch_bounds__(64 * KV8_WAVES, MT == 1 && HD <= 128 ? 4 : 2) void 
     }
 
     // ---- the waves of a workgroup, in wave order ----
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        l[mt] += __shfl_xor(l[mt], 16);
-        l[mt] += __shfl_xor(l[mt], 32);
-        if (g == 0) { m_all[wave][mt * 16 + c] = m[mt]; mo_all[wave][mt * 16 + c] = mo[mt]; l_all[wave][mt * 16 + c] = l[mt]; }
-    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (g == 0) { m_all[wave][c] = m; mo_all[wave][c] = mo; l_all[wave][c] = l; }
     __syncthreads();
-    float *dst = part + ((size_t)head * gridDim.y + blockIdx.y) * kv8_record(RG, HD);
+    float *dst = part + ((size_t)head * gridDim.y + blockIdx.y) * kv8_record(HD);
+    float M = -INFINITY, MO = -INFINITY, den = 0.f;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        float M = -INFINITY, MO = -INFINITY, den = 0.f;
+    for (int w = 0; w < KV8_WAVES; ++w) { M = fmaxf(M, m_all[w][c]); MO = fmaxf(MO, mo_all[w][c]); }
 #pragma unroll
-        for (int w = 0; w < KV8_WAVES; ++w) { M = fmaxf(M, m_all[w][mt * 16 + c]); MO = fmaxf(MO, mo_all[w][mt * 16 + c]); }
+    for (int w = 0; w < KV8_WAVES; ++w) {
+        const float mw = m_all[w][c], lw = l_all[w][c];
+        den += mw == -INFINITY ? lw : kv8_exp2(mw - M) * lw;         // (lw is zero there, or NaN)
+    }
+    const float mine = mo == -INFINITY ? 1.f : kv8_exp2(mo - MO), norm = kv8_exp2(MO - KV8_LIFT - M) / den;
+    const int r = r0 + c;
 #pragma unroll
-        for (int w = 0; w < KV8_WAVES; ++w) {
-            const float mw = m_all[w][mt * 16 + c], lw = l_all[w][mt * 16 + c];
-            den += mw == -INFINITY ? lw : kv8_exp2(mw - M) * lw;         // (lw is zero there, or NaN)
-        }
-        const float mine = mo[mt] == -INFINITY ? 1.f : kv8_exp2(mo[mt] - MO);
-        const int r = r0 + mt * 16 + c;
-        const float norm = kv8_exp2(MO - KV8_LIFT - M) / den;
+    for (int t0 = 0; t0 < DT; t0 += CH) {
+        if (t0) __syncthreads();
 #pragma unroll
-        for (int t0 = 0; t0 < DT; t0 += CH) {
-            if (mt || t0) __syncthreads();
+        for (int t = 0; t < CH; ++t) if (t0 + t < DT) o_slot[wave][t][lane] = o[t0 + t] * mine;
+        __syncthreads();
+        for (int t = wave; t < CH && t0 + t < DT; t += KV8_WAVES) {
+            f32x4 a = o_slot[0][t][lane];
 #pragma unroll
-            for (int t = 0; t < CH; ++t) if (t0 + t < DT) o_slot[wave][t][lane] = o[mt][t0 + t] * mine;
-            __syncthreads();
-            for (int t = wave; t < CH && t0 + t < DT; t += KV8_WAVES) {
-                f32x4 a = o_slot[0][t][lane];
-#pragma unroll
-                for (int w = 1; w < KV8_WAVES; ++w) a += o_slot[w][t][lane];
-                const int d = (t0 + t) * 16 + g * 4;
-                if (pt.splits > 1) kv8_put(dst + (mt * 16 + c) * HD + d, make_float4(a[0], a[1], a[2], a[3]));
-                else if (r < rows) kv8_out(out + ((size_t)b * pl.L + r / pl.group) * ldo + ((size_t)head * pl.group + r % pl.group) * HD + d, a * norm, vec & 2);
-            }
-        }
-        if (pt.splits > 1 && wave == 0 && g == 0) {
-            float *e = dst + RG * HD + mt * 16 + c;
-            e[0] = M; e[RG] = MO; e[2 * RG] = den;
+            for (int w = 1; w < KV8_WAVES; ++w) a += o_slot[w][t][lane];
+            const int d = (t0 + t) * 16 + g * 4;
+            if (r >= rows) continue;
+            if (pt.splits > 1) *reinterpret_cast<float4 *>(dst + c * HD + d) = make_float4(a[0], a[1], a[2], a[3]);
+            else kv8_out(out + ((size_t)b * pl.L + r / pl.group) * ldo + ((size_t)head * pl.group + r % pl.group) * HD + d, a * norm, vec & 2);
         }
     }
+    if (pt.splits > 1 && wave == 0 && g == 0 && r < rows) { dst[RG * HD + c] = M; dst[RG * HD + RG + c] = MO; dst[RG * HD + 2 * RG + c] = den; }
 }
 
 // Joins the splits of a pair.  64 units (four values of a row) a workgroup, KV8_JOIN threads each: a thread takes every KV8_JOIN-th split,
@@ -487,19 +460,19 @@ __global__ __launch_bounds__(64 * KV8_JOIN) void kv8_merge_kernel(const float *_
     __shared__ f32x4 acc[KV8_JOIN][64];
     Kv8Part pt;
     if (!kv8_part(pl, (int)blockIdx.y, true, pt) || pt.splits < 2) return;
-    const int head = blockIdx.x, b = pt.pair / pl.qgroups, r0 = (pt.pair - b * pl.qgroups) * pl.rg, rows = pl.L * pl.group;
-    const size_t rec = kv8_record(pl.rg, hd);
+    const int head = blockIdx.x, b = pt.pair / pl.qgroups, r0 = (pt.pair - b * pl.qgroups) * KV8_ROWS, rows = pl.L * pl.group;
+    const size_t rec = kv8_record(hd);
     const float *src = part + ((size_t)head * slots_total + pt.base) * rec;
     const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
     const int u = (int)blockIdx.z * 64 + x, lr = u / (hd / 4), d = u % (hd / 4) * 4, r = r0 + lr;
-    const bool live = lr < pl.rg && r < rows;
-    const float *e = src + pl.rg * hd + lr;
+    const bool live = lr < KV8_ROWS && r < rows;
+    const float *e = src + KV8_ROWS * hd + lr;
     float M = -INFINITY, MO = -INFINITY, den = 0.f;
     f32x4 a = {0.f, 0.f, 0.f, 0.f};
     if (live) {
 #pragma unroll 4
         for (int s = y; s < pt.splits; s += KV8_JOIN) {
-            const float ms = e[s * rec], mos = e[s * rec + pl.rg], ls = e[s * rec + 2 * pl.rg];
+            const float ms = e[s * rec], mos = e[s * rec + KV8_ROWS], ls = e[s * rec + 2 * KV8_ROWS];
             const float4 v = *reinterpret_cast<const float4 *>(src + s * rec + lr * hd + d);
             const float Mn = fmaxf(M, ms), MOn = fmaxf(MO, mos);
             den = (M == -INFINITY ? den : den * kv8_exp2(M - Mn)) + (ms == -INFINITY ? ls : ls * kv8_exp2(ms - Mn));
@@ -526,12 +499,11 @@ static int kv8_plan(int n_seqs, int L, int n_heads, int n_kv, int hd, int cap, K
 {
     if (!kv8_sizes(n_seqs, L, n_kv, hd, cap) || n_heads < n_kv || n_heads % n_kv || n_heads > KV8_MAX_HEADS) return SJD_EINVAL;
     const int64_t rows = (int64_t)L * (n_heads / n_kv);
-    const int rg = rows > 16 && hd <= 128 ? 32 : 16;       // (32 rows of heads of 256 do not fit 256 registers)
-    const int64_t pairs = n_seqs * ((rows + rg - 1) / rg);
-    if (rows > INT32_MAX - 64 || pairs > 65535) return SJD_EINVAL;
-    pl->n_seqs = n_seqs; pl->L = L; pl->group = n_heads / n_kv; pl->qgroups = (int)((rows + rg - 1) / rg); pl->rg = rg;
+    const int64_t pairs = n_seqs * ((rows + KV8_ROWS - 1) / KV8_ROWS);
+    if (rows > INT32_MAX - KV8_ROWS || pairs > 65535) return SJD_EINVAL;
+    pl->n_seqs = n_seqs; pl->L = L; pl->group = n_heads / n_kv; pl->qgroups = (int)((rows + KV8_ROWS - 1) / KV8_ROWS);
     pl->cap = cap; pl->nblk = (cap + 31) / 32;
-    pl->slots = pairs * n_kv >= 192 ? 0 : std::max(1, 256 / n_kv);
+    pl->slots = pairs * n_kv >= 192 || pl->nblk <= KV8_SHORT ? 0 : std::max(1, 256 / n_kv);
     *slots_total = (int)pairs + pl->slots;
     return SJD_OK;
 }
@@ -543,7 +515,7 @@ extern "C" int sjd_kv8_attention_workspace(int32_t n_seqs, int32_t L, int32_t n_
     Kv8Plan pl;
     int slots;
     SJD_TRY(kv8_plan(n_seqs, L, n_heads, n_kv_heads, head_dim, cap, &pl, &slots));
-    *bytes = pl.slots ? (size_t)slots * n_kv_heads * kv8_record(pl.rg, head_dim) * sizeof(float) : 0;
+    *bytes = pl.slots ? (size_t)slots * n_kv_heads * kv8_record(head_dim) * sizeof(float) : 0;
     return SJD_OK;
 }
 
@@ -564,22 +536,20 @@ extern "C" int sjd_kv8_attention(int32_t dtype, const void *q, int64_t ldq, cons
     const int vec = (mx_vec(q, ldq, dtype) ? 1 : 0) | ((uintptr_t)out % (dtype ? 8 : 16) == 0 && ldo % 4 == 0 ? 2 : 0);
     hipStream_t s = (hipStream_t)stream;
     const dim3 grid(n_kv_heads, slots);
-#define GO(HD, MT, T) SJD_LAUNCH((kv8_attention_kernel<HD, MT, T>), grid, dim3(64 * KV8_WAVES), 0, s, (const T *)q, ldq, cache, scales, pl, (T *)out, ldo, vec, (float *)workspace)
-#define GO1(HD, MT) do { if (dtype == 0) GO(HD, MT, float); else GO(HD, MT, bf16_t); } while (0)
-#define GO2(HD) do { if (pl.rg == 16) GO1(HD, 1); else if constexpr (HD <= 128) GO1(HD, 2); } while (0)
+#define GO1(HD, T) SJD_LAUNCH((kv8_attention_kernel<HD, T>), grid, dim3(64 * KV8_WAVES), 0, s, (const T *)q, ldq, cache, scales, pl, (T *)out, ldo, vec, (float *)workspace)
+#define GO(HD) do { if (dtype == 0) GO1(HD, float); else GO1(HD, bf16_t); } while (0)
     switch (head_dim) {
-        case 32: GO2(32); break;
-        case 64: GO2(64); break;
-        case 96: GO2(96); break;
-        case 128: GO2(128); break;
-        default: GO2(256); break;
+        case 32: GO(32); break;
+        case 64: GO(64); break;
+        case 96: GO(96); break;
+        case 128: GO(128); break;
+        default: GO(256); break;
     }
-#undef GO2
-#undef GO1
 #undef GO
+#undef GO1
     HIP_TRY(hipGetLastError());
     if (pl.slots) {
-        const int join = 64 * KV8_JOIN, units = std::min(pl.rg, pl.L * pl.group) * (head_dim / 4);
+        const int join = 64 * KV8_JOIN, units = std::min<int64_t>(KV8_ROWS, (int64_t)pl.L * pl.group) * (head_dim / 4);
         const dim3 mgrid(n_kv_heads, pl.n_seqs * pl.qgroups, (units + 63) / 64);
         if (dtype == 0) SJD_LAUNCH((kv8_merge_kernel<float>), mgrid, dim3(join), 0, s, (const float *)workspace, pl, head_dim, slots, (float *)out, ldo, vec);
         else SJD_LAUNCH((kv8_merge_kernel<bf16_t>), mgrid, dim3(join), 0, s, (const float *)workspace, pl, head_dim, slots, (bf16_t *)out, ldo, vec);

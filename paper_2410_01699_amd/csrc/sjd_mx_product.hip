@@ -56,23 +56,6 @@ template <int FMT, bool EXACT> __device__ __forceinline__ f32x4 mx_step(const ui
     return mx_mfma<FMT>(w, a0, a1, acc, ws, as);
 }
 
-// Buffer descriptors: scalar offsets, and loads whose vector offset lies behind the end give zeros and cost no memory access (scalar offsets
-// stay inside: the hardware takes them from the size before it compares).
-#define MX_OOB 0x40000000        // behind every buffer here
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_buffer(const uint8_t *p, size_t bytes)
-{
-    // (uniform, and said so: else every load becomes a loop over the wave's descriptors)
-    const uint64_t a = (uint64_t)p;
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
-    return __builtin_amdgcn_make_buffer_rsrc((void *)((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
-}
-__device__ __forceinline__ uint4 mx_load16(__amdgpu_buffer_rsrc_t r, int v, int s)
-{
-    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(r, v, s, 0);
-    return make_uint4(x[0], x[1], x[2], x[3]);
-}
-
 // ---- few rows -------------------------------------------------------------------------------
 // A workgroup owns TN tiles of features and up to 16 MT rows; its waves take the records of a tile in turn, so K is split eight ways, and their
 // sums meet in LDS in wave order.  A wave has one record of every tile (4 steps of 128 values) and its activations in flight: each
