@@ -89,8 +89,7 @@ __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const uint8_t *__restri
     auto load_scales = [&](int g) {
 #pragma unroll
         for (int t = 0; t < TN; ++t) wn[t] = __builtin_amdgcn_raw_buffer_load_b32(wb, lane * 4, (min(t, last) * groups + g) * MX_REC + 4096, 0);
-        // (a row's scales of four steps; a step at a time they would be as many lines as the activations themselves.  Behind K they are
-        // another row's, and meet weights of zero)
+        // (a row's scales of four steps; a step at a time they would be as many lines as the activations themselves)
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) an[mt] = mx_load16(sb, vs[mt], g * 16);
     };
@@ -148,7 +147,12 @@ __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const uint8_t *__restri
 #pragma unroll
         for (int t = 0; t < TN; ++t) ws[t] = wn[t];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) as[mt] = an[mt];
+        for (int mt = 0; mt < MT; ++mt) {                      // (behind K lie the next row's, which may be NaN's)
+            as[mt] = an[mt];
+            if (g * 4 + 1 >= steps) as[mt].y = 0;
+            if (g * 4 + 2 >= steps) as[mt].z = 0;
+            if (g * 4 + 3 >= steps) as[mt].w = 0;
+        }
 #pragma unroll
         for (int s = 0; s < 4; ++s) step(s);
     }

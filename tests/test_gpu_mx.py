@@ -270,6 +270,20 @@ def test_nan_stays_in_its_row_and_column(B, M, bits):
     assert torch.isnan(out[hit]).all() and torch.equal(out[~hit], ref[~hit])
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("M", [2, 20, 70, 300])
+@pytest.mark.parametrize("K", [100, 130, 640, 1500])
+def test_nan_blocks_of_a_row_leave_the_row_before_alone(B, K, M, dtype):
+    """K that ends inside a record of 512 values: what is read behind a row is the next row's"""
+    N = 96
+    gpu, a, w = operands(M, N, K, 4)
+    ref = product(B, gpu, M, N, K, 4, dtype)
+    scales = gpu[1].clone()
+    scales[1::2] = 255
+    out = product(B, (gpu[0], scales, gpu[2]), M, N, K, 4, dtype)
+    assert torch.isnan(out[1::2]).all() and torch.equal(out[::2], ref[::2])
+
+
 @pytest.mark.parametrize("M", [1, 16, 50, 200])
 def test_calls_agree_and_are_captured(B, M):
     """the same bits on another stream, and from replays of a graph with eager work between them"""
