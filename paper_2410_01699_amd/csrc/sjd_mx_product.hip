@@ -341,7 +341,7 @@ static MxPlan mx_plan(int M, int N, int K)
     auto take = [&](double t, const MxPlan &p) { if (t < cost) { cost = t; best = p; } };
     const int mt = M <= 16 ? 1 : 2;
     for (int tn : {1, 2, 3, 4, 6}) {
-        if (mt == 2 && tn == 6) continue;
+        if ((mt == 2 && tn == 6) || M > 32 * 65535) continue;          // (what a grid holds)
         const double wgs = std::ceil(tiles / tn) * std::ceil(M / (16.0 * mt)), n = std::ceil(wgs / 256);
         const double t = n * (0.6 + std::max(groups / 8.0, 0.4) * ((mt == 1 ? 1.5 : 3.4) + 0.6 * tn)) * (n > 1 && mt == 1 ? 0.85 : 1);
         // (where memory bounds both: the one with less beside it)
@@ -381,7 +381,6 @@ extern "C" int sjd_mx_product(int32_t format, const uint8_t *codes, const uint8_
     if (need && (!workspace || workspace_bytes < need || !mx_aligned(workspace))) return SJD_EINVAL;
     const int Kp = mx_up(K, 128), tiles = (int)(((int64_t)N + 15) / 16), groups = mx_groups(K);
     const MxPlan p = mx_plan(M, N, K);
-    if (p.kind < 0 && ((int64_t)M + 16 * p.mt - 1) / (16 * p.mt) > 65535) return SJD_EINVAL;
     const int vec = (uintptr_t)C % (dtype ? 8 : 16) == 0 && ldc % 4 == 0;
     hipStream_t s = (hipStream_t)stream;
     float *part = (float *)workspace;

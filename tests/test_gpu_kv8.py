@@ -265,6 +265,19 @@ def test_a_visible_nan_value_is_nan_where_it_is_seen(B):
     assert np.isnan(got[0, 0, 0, 9]) and np.isfinite(np.delete(got[0, 0, 0], 9)).all()
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_nan_in_one_split_of_a_long_walk(B, dtype):
+    def change(kv):
+        kv[0, 100, 1, 0, 9], kv[0, 200, 0, 1, 3] = float("nan"), float("nan")           # a value of head 0, a key of head 1
+
+    c = Pair(B, 1, 3, 64, 4096)
+    c.append([0], 4010, seed=75, change=change)
+    got, want, _, _ = c.attend([4000], 2, 3, dtype=dtype)
+    assert np.isnan(got[0, :, 0, 9]).all() and np.isfinite(np.delete(got[0, :, 0], 9, axis=-1)).all()
+    assert np.isnan(got[0, :, 1]).all() and np.isfinite(got[0, :, 2]).all()
+    c.check([4000], 2, 3, window=3000, sinks=32, dtype=dtype)                           # both hidden
+
+
 def test_a_bad_query_row_stays_alone(B):
     def change(q):
         q[3, 7], q[17, 20] = float("nan"), float("inf")
@@ -283,6 +296,60 @@ def test_rows_of_wider_matrices(B, pad):
     c.append([0, 0], 50, seed=71)
     for dtype in TYPES:
         c.check([30, 44], 5, 4, dtype=dtype, pad=pad)
+
+
+def test_caches_of_more_than_4_gib(B):
+    """the last sequence's last positions, seen through a window, give what a short cache gives that holds the same"""
+    n_seqs, n_kv, hd, cap, L, window = 3, 8, 256, 393216, 5, 70
+    assert n_seqs * n_kv * (cap // 32) * 64 * hd > 2 ** 32
+    big = (torch.zeros(n_seqs, n_kv, cap // 32, 64 * hd, dtype=torch.uint8, device="cuda"), torch.zeros(n_seqs, n_kv, cap // 32, 2, dtype=torch.uint8, device="cuda"))
+    c = Pair(B, 1, n_kv, hd, 192)
+    kv = rnd(90, 160, 2 * n_kv * hd)
+    end = cap - 192
+    for rows, small, large in ((kv[:160], [0], end), (rnd(91, L, 2 * n_kv * hd), [160], end + 160)):
+        k, v = (rows[:, i * n_kv * hd:(i + 1) * n_kv * hd].cuda() for i in range(2))
+        B.sjd_kv8_append(k, v, lengths(small), len(rows), n_kv, hd, 192, c.codes, c.scales)
+        every = torch.zeros(n_seqs * len(rows), 2 * n_kv * hd, device="cuda")
+        every[-len(rows):] = rows.cuda()
+        B.sjd_kv8_append(every[:, :n_kv * hd], every[:, n_kv * hd:], lengths([-1, -1, large]), len(rows), n_kv, hd, cap, *big)
+    q = rnd(92, n_seqs * L, n_kv * hd).cuda()
+    outs = []
+    for cache, n, m, x in (((c.codes, c.scales), [160], 192, q[-L:]), (big, [-1, -1, end + 160], cap, q)):
+        out = torch.full_like(x, 7.0)
+        ws = torch.empty(B.sjd_kv8_attention_workspace(len(n), L, n_kv, n_kv, hd, m), dtype=torch.uint8, device="cuda")
+        B.sjd_kv8_attention(x, *cache, lengths(n), L, n_kv, n_kv, hd, m, window, 0, out, ws)
+        outs.append(out)
+    assert (outs[1][:-L] == 7).all()
+    assert torch.equal(outs[0], outs[1][-L:])             # (the same blocks in the same order)
+
+
+def test_two_attentions_at_the_same_time(B):
+    """two streams with a cache and a workspace each, long enough to be split; an append to the one while the other is read"""
+    n_kv, hd, cap, n, L = 4, 64, 4096, 4000, 3
+    caches = [Pair(B, 1, n_kv, hd, cap) for _ in range(2)]
+    qs, ref, wss = [], [], []
+    need = B.sjd_kv8_attention_workspace(1, L, n_kv, n_kv, hd, cap)
+    assert need > 0
+    new = rnd(95, L, 2 * n_kv * hd).cuda()
+
+    def step(c, q, ws, out, stream):
+        B.sjd_kv8_append(new[:, :n_kv * hd], new[:, n_kv * hd:], length, L, n_kv, hd, cap, c.codes, c.scales, stream=stream)
+        B.sjd_kv8_attention(q, c.codes, c.scales, length, L, n_kv, n_kv, hd, cap, 0, 0, out, ws, stream=stream)
+
+    length = lengths([n])
+    for i, c in enumerate(caches):
+        c.append([0], n, seed=93 + i)
+        qs.append(rnd(97 + i, L, n_kv * hd).cuda())
+        wss.append(torch.empty(need, dtype=torch.uint8, device="cuda"))
+        ref.append(torch.empty_like(qs[-1]))
+        step(c, qs[-1], wss[-1], ref[-1], None)
+    outs, streams = [torch.zeros_like(r) for r in ref], [torch.cuda.Stream() for _ in ref]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, q, ws, out, s in zip(caches, qs, wss, outs, streams):
+            step(c, q, ws, out, s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, ref))
 
 
 def test_a_layer_step_is_captured_and_replayed(B):

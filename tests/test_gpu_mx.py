@@ -315,3 +315,91 @@ def test_calls_agree_and_are_captured(B, M):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(r, x)
+
+
+def test_matrices_of_more_than_4_gib(B):
+    """what lies behind 2^31 elements and 2^32 bytes: the last rows give what they give alone"""
+    K, dev = 1 << 16, "cuda"
+    x = torch.empty(33000, K, dtype=torch.bfloat16, device=dev)
+    x.view(torch.int16).random_(-0x3FFF, 0x3FFF)                       # (any finite bits below 2)
+    tail = x[-32:].contiguous()
+    codes, scales = buffers(*x.shape, 8)
+    few = buffers(32, K, 8)
+    B.sjd_mx_quantize(8, x, codes, scales)
+    B.sjd_mx_quantize(8, tail, *few)
+    assert torch.equal(codes[-32:], few[0]) and torch.equal(scales[-32:], few[1])
+    codes.zero_()
+    gain = torch.ones(K, device=dev)
+    B.sjd_mx_rmsnorm(8, x, None, gain, 1e-5, codes, scales)
+    B.sjd_mx_rmsnorm(8, tail, None, gain, 1e-5, *few)
+    assert torch.equal(codes[-32:], few[0]) and torch.equal(scales[-32:], few[1])
+    del codes, scales
+    packed, part = (torch.empty(B.sjd_mx_weights_bytes(n, K), dtype=torch.uint8, device=dev) for n in (33000, 24))
+    B.sjd_mx_weights(x, packed)
+    B.sjd_mx_weights(x[-24:], part)                                    # 33000 = 16 * 2061 + 24: whole tiles
+    assert torch.equal(packed[-part.numel():], part)
+
+
+@pytest.mark.parametrize("M,N,K,dtype", [(70000, 16390, 128, "fp32"), (2200000, 20, 200, "fp32"), (3, 2200000, 100, "fp32")])
+def test_products_of_very_many_rows_or_features(B, M, N, K, dtype):
+    """outputs of more than 4 GiB, more rows than a grid's second dimension holds; the last rows and features against the reference"""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, w = torch.randn(M, K, device="cuda", generator=g), torch.randn(N, K, device="cuda", generator=g)
+    codes, scales = buffers(M, K, 8)
+    packed = torch.empty(B.sjd_mx_weights_bytes(N, K), dtype=torch.uint8, device="cuda")
+    B.sjd_mx_quantize(8, x, codes, scales)
+    B.sjd_mx_weights(w, packed)
+    out = product(B, (codes, scales, packed), M, N, K, 8, dtype)
+    rows, cols = min(M, 40), min(N, 50)
+    a = R.values(codes[-rows:].cpu().numpy(), scales[-rows:].cpu().numpy(), 8)
+    v = R.values(*R.quantise(w[-cols:].cpu().double().numpy(), 4), 4)
+    check_product(out[-rows:, -cols:], a, v, K, dtype)
+
+
+def test_products_at_the_same_time(B):
+    """two streams, a workspace each, and a size that is split over K (so that both use theirs)"""
+    M, N, K = 128, 4096, 11008
+    assert B.sjd_mx_product_workspace(M, N, K) > 0
+    gpu = [operands(M, N, K, 8, seed=20 + i)[0] for i in range(2)]
+    ref = [product(B, x, M, N, K, 8, "fp32") for x in gpu]
+    outs, ws = [torch.zeros_like(r) for r in ref], [torch.empty(B.sjd_mx_product_workspace(M, N, K), dtype=torch.uint8, device="cuda") for _ in gpu]
+    streams = [torch.cuda.Stream() for _ in gpu]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, o, w, s in zip(gpu, outs, ws, streams):
+            B.sjd_mx_product(8, *x, K, o, w, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, r) for o, r in zip(outs, ref))
+
+
+def test_the_binding_refuses(B):
+    """sizes, types and layouts that do not fit each other"""
+    def e(*shape, dtype=torch.float32):
+        return torch.empty(*shape, dtype=dtype, device="cuda")
+
+    def u8(*shape):
+        return e(*shape, dtype=torch.uint8)
+
+    x, c, s, p, o = e(4, 64), u8(4, 128), u8(4, 4), u8(4352), e(4, 16)
+    cache, cs, n = u8(2, 1, 2, 64 * 64), u8(2, 1, 2, 2), torch.zeros(2, dtype=torch.int32, device="cuda")
+    bad = [lambda: B.sjd_mx_quantize(8, x, u8(4, 64), s), lambda: B.sjd_mx_quantize(8, x, c, u8(4, 2)), lambda: B.sjd_mx_quantize(5, x, c, s),
+           lambda: B.sjd_mx_quantize(8, x.half(), c, s), lambda: B.sjd_mx_quantize(8, x.t(), u8(64, 128), u8(64, 4)), lambda: B.sjd_mx_quantize(8, x[0], c, s),
+           lambda: B.sjd_mx_quantize(8, x, c.cpu(), s), lambda: B.sjd_mx_quantize(8, x, c.view(torch.int8), s), lambda: B.sjd_mx_quantize(8, x, c, s, up=x[:, :32]),
+           lambda: B.sjd_mx_quantize(8, x, c, s, up=x.bfloat16()), lambda: B.sjd_mx_quantize(8, x, c, s, up=e(4, 128)[:, :64]),
+           lambda: B.sjd_mx_quantize(8, x[:1].expand(4, 64), c, s), lambda: B.sjd_mx_quantize(8, x, u8(4, 256)[:, ::2], s),
+           lambda: B.sjd_mx_rmsnorm(8, x, x.bfloat16(), e(64), 1e-5, c, s), lambda: B.sjd_mx_rmsnorm(8, x, None, e(63), 1e-5, c, s),
+           lambda: B.sjd_mx_rmsnorm(8, x, e(3, 64), e(64), 1e-5, c, s), lambda: B.sjd_mx_rmsnorm(8, x, None, e(64), -1.0, c, s),
+           lambda: B.sjd_mx_weights(x, u8(4353)), lambda: B.sjd_mx_weights(x, u8(4336)),
+           lambda: B.sjd_mx_product(8, c, s, p, 129, o, None), lambda: B.sjd_mx_product(8, c, s, p, 64, e(4, 17), None), lambda: B.sjd_mx_product(4, c, s, p, 64, o, None),
+           lambda: B.sjd_mx_product(8, c, s, p, 64, e(5, 16), None), lambda: B.sjd_mx_product(8, u8(4 * 128 + 8)[8:].view(4, 128), s, p, 64, o, None),
+           lambda: B.sjd_kv8_append(e(4, 64), e(4, 64), n, 1, 1, 64, 64, cache, cs), lambda: B.sjd_kv8_append(e(2, 64), e(2, 64), n.long(), 1, 1, 64, 64, cache, cs),
+           lambda: B.sjd_kv8_append(e(2, 64), e(2, 64), n, 1, 1, 64, 65, cache, cs), lambda: B.sjd_kv8_append(e(2, 64), e(2, 65)[:, :64], n, 1, 1, 64, 64, cache, cs),
+           lambda: B.sjd_kv8_append(e(2, 64), e(2, 64), n[:0], 1, 1, 64, 64, cache, cs),
+           lambda: B.sjd_kv8_attention(e(2, 64), cache, cs, n, 1, 1, 1, 64, 64, 0, 0, e(2, 64, dtype=torch.bfloat16), None),
+           lambda: B.sjd_kv8_attention(e(2, 64), cache, cs, n, 1, 1, 1, 64, 64, -1, 0, e(2, 64), None),
+           lambda: B.sjd_kv8_attention(e(2, 64), cache, cs[:1], n, 1, 1, 1, 64, 64, 0, 0, e(2, 64), None),
+           lambda: B.sjd_kv8_attention(e(2, 64), u8(2, 1, 64, 64 * 64), u8(2, 1, 64, 2), n, 1, 1, 1, 64, 2048, 0, 0, e(2, 64), u8(64))]
+    for i, f in enumerate(bad):
+        with pytest.raises(B.SjdError) as err:
+            f()
+        assert err.value.code == B.SJD_EINVAL, i

@@ -40,7 +40,7 @@ REFUSED = [
                                 dict(hd=0), dict(hd=512, ld=2048), dict(cap=0), dict(cap=2 ** 31 - 1)]),
     ("sjd_kv8_attention", ATTEND, [dict(dtype=2), dict(q=None), dict(cache=None), dict(scales=None), dict(len=None), dict(out=None), dict(cache=ODD),
                                    dict(scales=ODD), dict(ldq=255), dict(ldo=255), dict(n_seqs=0), dict(L=0), dict(L=65), dict(heads=3), dict(heads=1),
-                                   dict(heads=0), dict(hd=80), dict(cap=0), dict(window=-1), dict(sinks=-1), dict(ws=None), dict(ws=ODD), dict(ws_bytes=16)]),
+                                   dict(heads=0), dict(hd=80), dict(cap=0), dict(window=-1), dict(sinks=-1), dict(ws=None, cap=2048), dict(ws=ODD, cap=2048), dict(ws_bytes=16, cap=2048)]),
 ]
 
 
@@ -58,8 +58,9 @@ def test_sizes():
         assert getattr(B._lib, f)(*bad, C.byref(n)) == BAD
     assert B._lib.sjd_mx_weights_bytes(1, 1, None) == BAD and B._lib.sjd_mx_product_workspace(1, 1, 1, None) == BAD
     assert B._lib.sjd_kv8_attention_workspace(1, 1, 1, 1, 64, 64, None) == BAD
-    # a workspace does not depend on how long the cache is
-    assert B.sjd_kv8_attention_workspace(1, 1, 8, 8, 128, 1 << 20) == B.sjd_kv8_attention_workspace(1, 1, 8, 8, 128, 64)
+    # a workspace does not grow with the cache, and short ones need none
+    assert B.sjd_kv8_attention_workspace(1, 1, 8, 8, 128, 1 << 20) == B.sjd_kv8_attention_workspace(1, 1, 8, 8, 128, 1025) > 0
+    assert B.sjd_kv8_attention_workspace(1, 1, 8, 8, 128, 1024) == 0
 
 
 def u8(n):
