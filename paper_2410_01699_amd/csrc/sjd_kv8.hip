@@ -159,6 +159,8 @@ extern "C" int sjd_kv8_append(int32_t dtype, const void *k, const void *v, int64
 // Where every walk has up to this many blocks none is split, four blocks a wave, and nothing is joined.  Cut and joined against whole: 9.6 us
 // against 6.6 (300 positions, one query, 32 heads), 10.1 against 8.4 (583, 16 queries); longer walks gain from the cut.
 #define KV8_SHORT 32
+#define KV8_NEAR_LIFT 12 // probabilities up to 2^KV8_HEADROOM times 2^12 in fp16: 22 bits of hi + lo hold from 2^-14 on, and 2^-37 below
+#define KV8_HEADROOM 3.f
 #define KV8_LIFT 14      // probabilities times 2^14 in fp16: 22 bits of hi + lo hold from 2^-27 of the largest on
 
 // The queries of one sequence that read one cache head, L * (heads per cache head) rows with a query's heads next to each other, are cut
@@ -230,10 +232,10 @@ __device__ __forceinline__ bool kv8_part(const Kv8Plan &pl, int want, bool by_pa
     return false;
 }
 
-__device__ __forceinline__ f16x8 kv8_f16(uint32_t lo, uint32_t hi)        // eight codes
+__device__ __forceinline__ f16x8 kv8_f16(uint32_t lo, uint32_t hi, float scale = 1.f)        // eight codes, times a power of two
 {
-    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
-    const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
+    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, true);
+    const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, true);
     return (f16x8){a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
 // bytes 0x80 where a code is NaN (0x7F with any sign)
@@ -265,9 +267,14 @@ __device__ __forceinline__ void kv8_out(bf16_t *p, const f32x4 &v, bool vec)
 
 // Per block of 32 positions, with the scales 2^ek and 2^ev of its keys and values:
 //   S^T[key][row] = K codes . Q (Q scaled per row to 2^13 .. 2^14, hi + lo fp16)        s = S * 2^ek * 2^eq * log2(e) / sqrt(HD)
-//   m = max s, l = sum 2^(s - m);   mo = max (s + ev):  O = sum 2^(s + ev - mo + LIFT) * V codes
-// O has a reference of its own because the blocks' scales differ: with it the largest contribution is always 2^LIFT, whatever the
-// scales are, and fp16 holds what matters beside it.  out = O * 2^(mo - LIFT - m) / l.
+//   l = sum 2^(s - m),   O = sum 2^(s + ev - mo + KV8_LIFT) * V codes,   out = O * 2^(mo - KV8_LIFT - m) / l
+// with references m and mo that may be any numbers near the largest s and s + ev: O has one of its own because the blocks' scales differ, so
+// that fp16 holds its largest contributions whatever the scales are.
+// Most walks need less.  While the value scales are within a few powers of two of the wave's first one, the codes take the difference when they
+// become fp16 (exactly: 2^-9 2^-5 .. 448 2^6), O keeps to m, and m stays until a score is 2^KV8_HEADROOM above it: what is left of a block beside
+// its conversions (64 codes a lane) is 8 exponentials, their sum and a comparison.  Against references that follow every block: 38.7 us
+// against 43.8 (32 queries x 4 heads a cache head, 16 k positions), 15.2 against 16.3 (8 x 16 queries of 32 heads), 19.9 against 22.2
+// (128 queries, 4 k positions); no difference where memory bounds, one query.
 // The two score tiles of a block leave lane (g, c) with row c and the positions 16 h + 4 g + i: the order in which V's operands hold them.
 template <int HD, typename T>
 __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attention_kernel(const T *__restrict__ q, int64_t ldq, const uint8_t *__restrict__ cache,
@@ -294,16 +301,17 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
     uint4 ka[KS], va[KS];
     int sc = 0;
     auto place = [&](int v) { return v < sp.front ? v : sp.first + v - sp.front; };
-    auto fetch_k = [&](int blk) {
-        const auto rec = mx_buffer(cache + (at0 + blk) * (64 * HD), 64 * HD);      // (a descriptor in scalars: one register of lane offsets)
+    auto fetch_k = [&](int v) {                                    // (behind the end: nothing is read)
+        const int blk = place(min(v, v_end - 1));
+        const auto rec = mx_buffer(cache + (at0 + blk) * (64 * HD), v < v_end ? 64 * HD : 0);      // (a descriptor in scalars: one register of lane offsets)
 #pragma unroll
-        for (int p = 0; p < KS; ++p) ka[p] = mx_load16(rec, lane * 16, p * 1024);
+        for (int p = 0; p < KS; ++p) ka[p] = mx_load16(rec, lane * 16 + p * 1024, 0);
         sc = *reinterpret_cast<const uint16_t *>(scales + (at0 + blk) * 2);
     };
-    auto fetch_v = [&](int blk) {
-        const auto rec = mx_buffer(cache + (at0 + blk) * (64 * HD), 64 * HD);
+    auto fetch_v = [&](int v) {
+        const auto rec = mx_buffer(cache + (at0 + place(min(v, v_end - 1))) * (64 * HD), v < v_end ? 64 * HD : 0);
 #pragma unroll
-        for (int p = 0; p < KS; ++p) va[p] = mx_load16(rec, lane * 16, (KS + p) * 1024);
+        for (int p = 0; p < KS; ++p) va[p] = mx_load16(rec, lane * 16 + (KS + p) * 1024, 0);
     };
     int v = v_beg + wave;
     // Q by wave 0: lane (g, c) has values 32 ks + 8 g .. of row c.  Requested first: loads return in order.
@@ -315,7 +323,8 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
         for (int ks = 0; ks < KS; ++ks) mx_load8<T>(src, ks * 32 + g * 8, HD, vec & 1, x[ks]);
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (v < v_end) { fetch_k(place(v)); fetch_v(place(v)); }
+    fetch_k(v);
+    fetch_v(v);
     __builtin_amdgcn_sched_barrier(0);
 
     if (wave == 0) {
@@ -347,15 +356,17 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
     f32x4 o[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, mo = -INFINITY, l = 0.f;
+    float m = -INFINITY, mo, l = 0.f;
     const float qs = q_scale[c];
     const int pos = sp.n + min(r0 + c, rows - 1) / pl.group;
-    auto block = [&](auto more) {
-        const int blk = place(v), k0 = blk * 32, next = more.value ? place(v + KV8_WAVES) : 0;
-        const int sb = __builtin_amdgcn_readfirstlane(sc);
-        const float ks2 = mx_pow2(sb & 255), ev = (float)((sb >> 8) - 127);
-        const bool whole = k0 + 31 <= sp.n + sp.i0 && (!pl.window || k0 > sp.n + sp.i1 - pl.window || k0 + 31 < pl.sinks);
-        f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    // S = K codes . Q, then the next block's keys are requested; whole: no row's mask hides anything of the block
+    f32x4 s[2];
+    int k0 = 0, sb = 0;
+    bool whole = true;
+    auto scores = [&]() {
+        k0 = place(v) * 32;
+        whole = k0 + 31 <= sp.n + sp.i0 && (!pl.window || k0 > sp.n + sp.i1 - pl.window || k0 + 31 < pl.sinks);
+        s[0] = s[1] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int op = 0; op < 2 * KS; ++op) {
             const f16x8 k = (op & 1) ? kv8_f16(ka[op / 2].z, ka[op / 2].w) : kv8_f16(ka[op / 2].x, ka[op / 2].y);
@@ -363,53 +374,15 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
             for (int p = PL - 1; p >= 0; --p) s[op / KS] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q_lds[op % KS][p][lane], s[op / KS], 0, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (more.value) { fetch_k(next); __builtin_amdgcn_sched_barrier(0); }
-        f16x8 ph, plo;
-        uint32_t seen = 0xFFu;
-        const float cs = qs * ks2;
-        float x[8], bm;
-        if (whole) {
-            bm = s[0][0];
-#pragma unroll
-            for (int e = 1; e < 8; ++e) bm = fmaxf(bm, s[e >> 2][e & 3]);
-            bm *= cs;
-        } else {
-            bm = -INFINITY;
-            seen = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int key = k0 + (e >> 2) * 16 + g * 4 + (e & 3);
-                const bool see = (key <= pos) & ((pl.window == 0) | (key > pos - pl.window) | (key < pl.sinks));
-                seen |= see ? 1u << e : 0u;
-                x[e] = see ? s[e >> 2][e & 3] * cs : -INFINITY;
-                bm = fmaxf(bm, x[e]);
-            }
-        }
-        bm = kv8_across(bm);
-        const float mn = fmaxf(m, bm), mon = fmaxf(mo, bm + ev);
-        const float so = mn == -INFINITY ? 1.f : kv8_exp2(m - mn);
-        const float f = mn == -INFINITY ? 0.f : kv8_exp2(fminf(ev - mon + mn + KV8_LIFT, 120.f));
-        const float turn = mon == -INFINITY ? 1.f : kv8_exp2(mo - mon);      // what the output so far is rescaled by
-        if (whole) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = kv8_exp2(fmaf(s[e >> 2][e & 3], cs, -mn));
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = seen >> e & 1 ? kv8_exp2(x[e] - mn) : 0.f;
-        }
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            sum += x[e];
-            float pf = x[e] * f;
-            if (PL == 2) asm("" : "+v"(pf));     // (the product in fp32 for both parts: fused into the conversion to fp16 it rounds otherwise now and then)
-            ph[e] = (_Float16)pf;
-            if (PL == 2) plo[e] = (_Float16)(pf - (float)ph[e]);
-        }
-        l = l * so + sum;
-        m = mn; mo = mon;
-#pragma unroll
-        for (int t = 0; t < DT; ++t) o[t] *= turn;
+        fetch_k(v + KV8_WAVES);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto sees = [&](int e) {
+        const int key = k0 + (e >> 2) * 16 + g * 4 + (e & 3);
+        return (key <= pos) & ((pl.window == 0) | (key > pos - pl.window) | (key < pl.sinks));
+    };
+    // O += V codes times `scale` . P, then the next block's values are requested
+    auto weigh = [&](const f16x8 &ph, const f16x8 &plo, uint32_t seen, float scale) {
         if (!whole) {
             // Zero times NaN is NaN: where a mask may hide a NaN code from some row, the codes are taken out, and the rows that see one
             // get it by counting.
@@ -437,15 +410,102 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
         }
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
-            const f16x8 vv = (t & 1) ? kv8_f16(va[t / 2].z, va[t / 2].w) : kv8_f16(va[t / 2].x, va[t / 2].y);
+            const f16x8 vv = (t & 1) ? kv8_f16(va[t / 2].z, va[t / 2].w, scale) : kv8_f16(va[t / 2].x, va[t / 2].y, scale);
             if (PL == 2) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, plo, o[t], 0, 0, 0);
             o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, ph, o[t], 0, 0, 0);
         }
-        if constexpr (more.value) { __builtin_amdgcn_sched_barrier(0); fetch_v(next); }
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_v(v + KV8_WAVES);
     };
-    if (v < v_end) {
-        for (; v + KV8_WAVES < v_end; v += KV8_WAVES) block(std::true_type{});
-        block(std::false_type{});
+    // ---- value scales near the first one ----
+    sb = __builtin_amdgcn_readfirstlane(sc);
+    const int base = sb >> 8;
+    float shift = KV8_NEAR_LIFT;                 // KV8_NEAR_LIFT - m, or without m while nothing is seen
+    for (; v < v_end; v += KV8_WAVES) {
+        sb = __builtin_amdgcn_readfirstlane(sc);
+        const int up = (sb >> 8) - base;
+        if (up < -5 || up > 6) break;
+        scores();
+        const float cs = qs * mx_pow2(sb & 255);
+        float x[8], bm;
+        uint32_t seen = 0xFFu;
+        if (whole) {
+            bm = s[0][0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) bm = fmaxf(bm, s[e >> 2][e & 3]);
+            bm *= cs;
+        } else {
+            bm = -INFINITY;
+            seen = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool see = sees(e);
+                seen |= see ? 1u << e : 0u;
+                x[e] = see ? s[e >> 2][e & 3] * cs : -INFINITY;
+                bm = fmaxf(bm, x[e]);
+            }
+        }
+        if (__ballot(bm > m + KV8_HEADROOM)) {
+            const float mn = fmaxf(m, kv8_across(bm)), turn = mn == -INFINITY ? 1.f : kv8_exp2(m - mn);
+            l *= turn;
+#pragma unroll
+            for (int t = 0; t < DT; ++t) o[t] *= turn;
+            m = mn;
+            shift = mn == -INFINITY ? KV8_NEAR_LIFT : KV8_NEAR_LIFT - mn;
+        }
+        if (whole) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = kv8_exp2(fmaf(s[e >> 2][e & 3], cs, shift));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = kv8_exp2(x[e] + shift);
+        }
+        f16x8 ph, plo = {};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            l += x[e];
+            ph[e] = (_Float16)x[e];
+            if (PL == 2) plo[e] = (_Float16)(x[e] - (float)ph[e]);
+        }
+        weigh(ph, plo, seen, mx_pow2(127 + up));
+    }
+    l *= mx_pow2(127 - KV8_NEAR_LIFT);
+    mo = m + (float)(base - 127 + KV8_LIFT - KV8_NEAR_LIFT);
+    // ---- the rest of a walk whose value scales differ by more ----
+    for (; v < v_end; v += KV8_WAVES) {
+        sb = __builtin_amdgcn_readfirstlane(sc);
+        scores();
+        const float cs = qs * mx_pow2(sb & 255), ev = (float)((sb >> 8) - 127);
+        float x[8], bm = -INFINITY;
+        uint32_t seen = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bool see = whole || sees(e);
+            seen |= see ? 1u << e : 0u;
+            x[e] = see ? s[e >> 2][e & 3] * cs : -INFINITY;
+            bm = fmaxf(bm, x[e]);
+        }
+        bm = kv8_across(bm);
+        const float mn = fmaxf(m, bm), mon = fmaxf(mo, bm + ev);
+        const float so = mn == -INFINITY ? 1.f : kv8_exp2(m - mn);
+        const float f = mn == -INFINITY ? 0.f : kv8_exp2(fminf(ev - mon + mn + KV8_LIFT, 120.f));
+        const float turn = mon == -INFINITY ? 1.f : kv8_exp2(mo - mon);      // what the output so far is rescaled by
+        float sum = 0.f;
+        f16x8 ph, plo = {};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[e] = seen >> e & 1 ? kv8_exp2(x[e] - mn) : 0.f;
+            sum += x[e];
+            float pf = x[e] * f;
+            if (PL == 2) asm("" : "+v"(pf));     // (the product in fp32 for both parts: fused into the conversion to fp16 it rounds otherwise now and then)
+            ph[e] = (_Float16)pf;
+            if (PL == 2) plo[e] = (_Float16)(pf - (float)ph[e]);
+        }
+        l = l * so + sum;
+        m = mn; mo = mon;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[t] *= turn;
+        weigh(ph, plo, seen, 1.f);
     }
 
     // ---- the waves of a workgroup, in wave order ----

@@ -217,6 +217,47 @@ def test_scales_of_blocks_far_apart(B):
         c.check([190], 2, 2, window=20)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("hd,heads", [(64, 1), (128, 3)])
+@pytest.mark.parametrize("kind", ["rising", "falling", "large and unlikely", "any"])
+def test_value_scales_that_leave_their_neighbourhood(B, kind, hd, heads, dtype):
+    """Several blocks to a wave, whose value scales wander off from the first one's.  The error is held to the mean of |v| under the
+    probabilities: those are off as above, and a sum of n products in fp32 by n 2^-24 of it."""
+    n, L, blocks = 1000, 3, 32
+    r = np.random.RandomState(7)
+    ev = {"rising": 1.5 * np.arange(blocks), "falling": -1.5 * np.arange(blocks), "large and unlikely": 24 * (np.arange(blocks) >= 12), "any": r.randint(-40, 40, blocks)}[kind]
+    ev = np.floor(ev)
+
+    def change(kv):
+        for blk in range(blocks):
+            kv[:, 32 * blk:32 * blk + 32, 1] *= 2.0 ** ev[blk]
+        kv[:, :, 0, :, 0] = 0.0
+        if kind == "large and unlikely":                        # scores lower by 20 log 2 or so (queries have 8 there)
+            kv[:, 32 * 12:, 0, :, 0] = -20 * np.log(2) * hd ** 0.5 / 8
+
+    def eight(q):
+        q[:, ::hd] = 8.0
+
+    c = Pair(B, 1, 1, hd, 1024)
+    c.append([0], n + L, seed=76, change=change)
+    got, want, mag, _ = c.attend([n], L, heads, dtype=dtype, change=eight)
+
+    class Magnitudes:
+        codes, hd, cap = c.ref.codes, c.ref.hd, c.ref.cap
+
+        def values(self, *a):
+            k, v = c.ref.values(*a)
+            return k, np.abs(v)
+
+    q = rnd(5, L, heads * hd)
+    eight(q)
+    mean, _, _ = R.attention(Magnitudes(), q.to(TYPES[dtype]).double().numpy().reshape(1, L, heads, hd), [n], L, heads, 0, 0)
+    d = (2.0 ** -22 + (hd + 8) * 2.0 ** -24) * mag
+    room = (np.expm1(2 * d) + 2.0 ** -20 + (n + L) * 2.0 ** -24 + (2.0 ** -11 if dtype == "bf16" else 0)) * mean
+    room = room + (2.0 ** -8 * (np.abs(want) + room) if dtype == "bf16" else 0)
+    assert np.isfinite(got).all() and (np.abs(got - want) <= room).all(), np.max(np.abs(got - want) / room)
+
+
 def test_queries_of_any_magnitude(B):
     def change(q):
         q[0] *= 2.0 ** -100
