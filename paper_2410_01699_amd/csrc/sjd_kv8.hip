@@ -159,6 +159,7 @@ extern "C" int sjd_kv8_append(int32_t dtype, const void *k, const void *v, int64
 // Where every walk has up to this many blocks none is split, four blocks a wave, and nothing is joined.  Cut and joined against whole: 9.6 us
 // against 6.6 (300 positions, one query, 32 heads), 10.1 against 8.4 (583, 16 queries); longer walks gain from the cut.
 #define KV8_SHORT 32
+#define KV8_SKEW 256     // blocks of a cache whose walks may differ by more than a second launch costs
 #define KV8_NEAR_LIFT 12 // probabilities up to 2^KV8_HEADROOM times 2^12 in fp16: 22 bits of hi + lo hold from 2^-14 on, and 2^-37 below
 #define KV8_HEADROOM 3.f
 #define KV8_LIFT 14      // probabilities times 2^14 in fp16: 22 bits of hi + lo hold from 2^-27 of the largest on
@@ -167,13 +168,14 @@ extern "C" int sjd_kv8_append(int32_t dtype, const void *k, const void *v, int64
 // into groups of 16 rows.  A (sequence, group) pair walks the blocks that any of its queries sees, the sinks' first.  Where the pairs are too
 // few for the chip their walks are cut into splits, all of about the same number of blocks: lengths live on the device, so the kernels work
 // the cut out themselves, every workgroup the same.
-// What more rows a workgroup gain: two tiles of rows per wave 40.5 us against 42.8 at 32 queries x 4 heads a cache head, 16 k positions, but 29
-// against 22 at 128 queries of one head, 4 k positions (half the workgroups); four to eight tiles over codes made fp16 once in LDS, 50 to 58.
+// More rows to a workgroup read less from L2, but leave fewer waves on a CU.  Two tiles of rows a wave: 35.4 us against 38.8 at 32 queries x 4 heads a
+// cache head and 16 k positions, where a head's records are read 8 times (15 TB/s), but 28.5 against 22.5 at 4 x 8 queries, 40.6 against 34.9 for
+// a prompt of 1000; four to eight tiles over codes made fp16 once in LDS, 50 to 58 for the first.
 struct Kv8Plan {
     const int32_t *len;
     int32_t n_seqs, L, group, qgroups;     // heads per cache head; row groups of KV8_ROWS rows per sequence
     int32_t window, sinks, cap, nblk;
-    int32_t slots;                             // splits to aim for per cache head; 0: one per pair, none cut
+    int32_t slots, least;                      // splits to aim for per cache head, of so many blocks at least; 0: one per pair, none cut
 };
 struct Kv8Span { int32_t i0, i1, n, first, front, count; };    // queries, cached positions; block v is v < front ? v : first + v - front
 __device__ __forceinline__ Kv8Span kv8_span(const Kv8Plan &pl, int pair)
@@ -210,7 +212,7 @@ __device__ __forceinline__ bool kv8_part(const Kv8Plan &pl, int want, bool by_pa
         for (int o = 1; o < min(pairs, 64); o <<= 1) c += __shfl_xor(c, o);
         total += __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(c)));
     }
-    part.per = cut ? max(KV8_WAVES, (int)ceilf(total / (float)pl.slots)) : KV8_SHORT;
+    part.per = cut ? max(pl.least, (int)ceilf(total / (float)pl.slots)) : KV8_SHORT;
     int base = 0;
     for (int p0 = 0; p0 < pairs; p0 += 64) {
         const int c = p0 == 0 ? c0 : p0 + lane < pairs ? kv8_span(pl, p0 + lane).count : 0;
@@ -597,7 +599,14 @@ static int kv8_plan(int n_seqs, int L, int n_heads, int n_kv, int hd, int cap, K
     if (rows > INT32_MAX - KV8_ROWS || pairs > 65535) return SJD_EINVAL;
     pl->n_seqs = n_seqs; pl->L = L; pl->group = n_heads / n_kv; pl->qgroups = (int)((rows + KV8_ROWS - 1) / KV8_ROWS);
     pl->cap = cap; pl->nblk = (cap + 31) / 32;
-    pl->slots = pairs * n_kv >= 192 || pl->nblk <= KV8_SHORT ? 0 : std::max(1, 256 / n_kv);
+    // Too few workgroups: splits for 256.  (512: 15.0 us against 13.7, one query, 4 k positions; splits up to 384 pairs and heads: 25.5 against 15.3,
+    // 8 x 16 queries of 32 heads.)
+    // Enough, but windows over long caches, of which one sequence may hold most: walks longer than 5/4 of the mean are cut.  One sequence of 30 k
+    // positions and seven of 100, 32 heads: 45.6 us against 102; eight of 2000, where it only costs the second launch, 27.1 against 23.8.  (Prompts have
+    // many groups of rows, which even out by themselves: 38 against 63; and every workgroup looks at all pairs.)
+    const bool few = pairs * n_kv < 192, skew = pl->nblk > KV8_SKEW && rows <= 32 && pairs <= 256;
+    pl->slots = pl->nblk <= KV8_SHORT ? 0 : few ? std::max(1, 256 / n_kv) : skew ? ((int)pairs * 4 + 4) / 5 : 0;
+    pl->least = few ? KV8_WAVES : KV8_SHORT;
     *slots_total = (int)pairs + pl->slots;
     return SJD_OK;
 }

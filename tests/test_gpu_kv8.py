@@ -198,6 +198,20 @@ def test_pairs_that_fill_the_chip_are_not_split(B):
     c.check([65 - 3 * i for i in range(16)], 1, 32)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_one_long_sequence_among_short_ones(B, dtype):
+    """pairs enough to fill the chip, of which one holds most of the positions: its walk is cut"""
+    n_seqs, n_kv, hd, cap = 5, 48, 32, 8224
+    assert B.sjd_kv8_attention_workspace(n_seqs, 2, n_kv, n_kv, hd, cap) > 0 == B.sjd_kv8_attention_workspace(n_seqs, 40, n_kv, n_kv, hd, cap)
+    c = Pair(B, n_seqs, n_kv, hd, cap)
+    c.append([-1, -1, 0, -1, -1], 3000, seed=73)                  # (append in pieces: the reference's arrays)
+    c.append([-1, -1, 3000, -1, -1], 3000, seed=74)
+    c.append([0, 0, -1, 0, 0], 300, seed=75)
+    for n in ([40, 299, 5998, 0, -1], [7, 200, 100, 0, 298]):     # (the second: nothing to cut)
+        c.check(n, 2, n_kv, dtype=dtype)
+    c.check([40, 299, 5998, 0, 250], 2, n_kv, window=2500, sinks=40, dtype=dtype)
+
+
 def test_scales_of_blocks_far_apart(B):
     """keys and values of whole blocks far smaller and larger than their neighbours', and blocks of zeros"""
     def change(kv):
