@@ -174,17 +174,21 @@ extern "C" int sjd_kv8_append(int32_t dtype, const void *k, const void *v, int64
 struct Kv8Plan {
     const int32_t *len;
     int32_t n_seqs, L, group, qgroups;     // heads per cache head; row groups of KV8_ROWS rows per sequence
+    int32_t group_shift, qgroups_shift;    // their logarithms, or -1 where they are no powers of two
     int32_t window, sinks, cap, nblk;
     int32_t slots, least;                      // splits to aim for per cache head, of so many blocks at least; 0: one per pair, none cut
 };
+__device__ __forceinline__ int kv8_div(int x, int d, int shift) { return shift >= 0 ? x >> shift : x / d; }     // (a division is 20 instructions in a row)
+__device__ __forceinline__ int kv8_query(const Kv8Plan &pl, int row) { return kv8_div(row, pl.group, pl.group_shift); }
+__device__ __forceinline__ int kv8_seq(const Kv8Plan &pl, int pair) { return kv8_div(pair, pl.qgroups, pl.qgroups_shift); }
 struct Kv8Span { int32_t i0, i1, n, first, front, count; };    // queries, cached positions; block v is v < front ? v : first + v - front
 __device__ __forceinline__ Kv8Span kv8_span(const Kv8Plan &pl, int pair)
 {
     Kv8Span s;
-    const int b = pair / pl.qgroups, r0 = (pair - b * pl.qgroups) * KV8_ROWS;
+    const int b = kv8_seq(pl, pair), r0 = (pair - b * pl.qgroups) * KV8_ROWS;
     s.n = pl.len[b];
-    s.i0 = r0 / pl.group;
-    s.i1 = min(r0 + KV8_ROWS - 1, pl.L * pl.group - 1) / pl.group;
+    s.i0 = kv8_query(pl, r0);
+    s.i1 = kv8_query(pl, min(r0 + KV8_ROWS - 1, pl.L * pl.group - 1));
     s.first = s.front = s.count = 0;
     if (s.n < 0 || s.n > pl.cap - pl.L) return s;
     const int last = s.n + s.i1;
@@ -296,7 +300,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
     if (!sp.count) return;
     const int per = pl.slots ? pt.per : sp.count;
     const int v_beg = pt.split * per, v_end = min(sp.count, v_beg + per);
-    const int b = pt.pair / pl.qgroups, r0 = (pt.pair - b * pl.qgroups) * RG, rows = pl.L * pl.group;
+    const int b = kv8_seq(pl, pt.pair), r0 = (pt.pair - b * pl.qgroups) * RG, rows = pl.L * pl.group;
 
     // The next block's keys are requested when this block's have left their registers, its values likewise.
     const size_t at0 = ((size_t)b * heads + head) * pl.nblk;
@@ -320,7 +324,8 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
     float x[KS][8];
     if (wave == 0) {
         const int r = min(r0 + c, rows - 1);
-        const T *src = q + ((size_t)b * pl.L + r / pl.group) * ldq + ((size_t)head * pl.group + r % pl.group) * HD;
+        const int i = kv8_query(pl, r);
+        const T *src = q + ((size_t)b * pl.L + i) * ldq + ((size_t)head * pl.group + (r - i * pl.group)) * HD;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) mx_load8<T>(src, ks * 32 + g * 8, HD, vec & 1, x[ks]);
     }
@@ -360,7 +365,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
     for (int t = 0; t < DT; ++t) o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, mo, l = 0.f;
     const float qs = q_scale[c];
-    const int pos = sp.n + min(r0 + c, rows - 1) / pl.group;
+    const int pos = sp.n + kv8_query(pl, min(r0 + c, rows - 1));
     // S = K codes . Q, then the next block's keys are requested; whole: no row's mask hides anything of the block
     f32x4 s[2];
     int k0 = 0, sb = 0;
@@ -525,7 +530,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
         den += mw == -INFINITY ? lw : kv8_exp2(mw - M) * lw;         // (lw is zero there, or NaN)
     }
     const float mine = mo == -INFINITY ? 1.f : kv8_exp2(mo - MO), norm = kv8_exp2(MO - KV8_LIFT - M) / den;
-    const int r = r0 + c;
+    const int r = r0 + c, i = kv8_query(pl, r);
 #pragma unroll
     for (int t0 = 0; t0 < DT; t0 += CH) {
         if (t0) __syncthreads();
@@ -539,7 +544,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
             const int d = (t0 + t) * 16 + g * 4;
             if (r >= rows) continue;
             if (pt.splits > 1) *reinterpret_cast<float4 *>(dst + c * HD + d) = make_float4(a[0], a[1], a[2], a[3]);
-            else kv8_out(out + ((size_t)b * pl.L + r / pl.group) * ldo + ((size_t)head * pl.group + r % pl.group) * HD + d, a * norm, vec & 2);
+            else kv8_out(out + ((size_t)b * pl.L + i) * ldo + ((size_t)head * pl.group + (r - i * pl.group)) * HD + d, a * norm, vec & 2);
         }
     }
     if (pt.splits > 1 && wave == 0 && g == 0 && r < rows) { dst[RG * HD + c] = M; dst[RG * HD + RG + c] = MO; dst[RG * HD + 2 * RG + c] = den; }
@@ -556,7 +561,7 @@ __global__ __launch_bounds__(64 * KV8_JOIN) void kv8_merge_kernel(const float *_
     __shared__ f32x4 acc[KV8_JOIN][64];
     Kv8Part pt;
     if (!kv8_part(pl, (int)blockIdx.y, true, pt) || pt.splits < 2) return;
-    const int head = blockIdx.x, b = pt.pair / pl.qgroups, r0 = (pt.pair - b * pl.qgroups) * KV8_ROWS, rows = pl.L * pl.group;
+    const int head = blockIdx.x, b = kv8_seq(pl, pt.pair), r0 = (pt.pair - b * pl.qgroups) * KV8_ROWS, rows = pl.L * pl.group;
     const size_t rec = kv8_record(hd);
     const float *src = part + ((size_t)head * slots_total + pt.base) * rec;
     const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
@@ -588,7 +593,8 @@ __global__ __launch_bounds__(64 * KV8_JOIN) void kv8_merge_kernel(const float *_
         a = a * (MO == -INFINITY ? 1.f : kv8_exp2(MO - MOn)) + acc[i][x] * (mos == -INFINITY ? 1.f : kv8_exp2(mos - MOn));
         M = Mn; MO = MOn;
     }
-    kv8_out(out + ((size_t)b * pl.L + r / pl.group) * ldo + ((size_t)head * pl.group + r % pl.group) * hd + d, a * (kv8_exp2(MO - KV8_LIFT - M) / den), vec & 2);
+    const int i = kv8_query(pl, r);
+    kv8_out(out + ((size_t)b * pl.L + i) * ldo + ((size_t)head * pl.group + (r - i * pl.group)) * hd + d, a * (kv8_exp2(MO - KV8_LIFT - M) / den), vec & 2);
 }
 
 static int kv8_plan(int n_seqs, int L, int n_heads, int n_kv, int hd, int cap, Kv8Plan *pl, int *slots_total)
@@ -598,6 +604,8 @@ static int kv8_plan(int n_seqs, int L, int n_heads, int n_kv, int hd, int cap, K
     const int64_t pairs = n_seqs * ((rows + KV8_ROWS - 1) / KV8_ROWS);
     if (rows > INT32_MAX - KV8_ROWS || pairs > 65535) return SJD_EINVAL;
     pl->n_seqs = n_seqs; pl->L = L; pl->group = n_heads / n_kv; pl->qgroups = (int)((rows + KV8_ROWS - 1) / KV8_ROWS);
+    auto shift = [](int d) { return d & (d - 1) ? -1 : __builtin_ctz(d); };
+    pl->group_shift = shift(pl->group); pl->qgroups_shift = shift(pl->qgroups);
     pl->cap = cap; pl->nblk = (cap + 31) / 32;
     // Too few workgroups: splits for 256.  (512: 15.0 us against 13.7, one query, 4 k positions; splits up to 384 pairs and heads: 25.5 against 15.3,
     // 8 x 16 queries of 32 heads.)
