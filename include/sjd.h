@@ -343,7 +343,8 @@ int sjd_gemm_bench(int32_t M, int32_t N, int32_t K, int32_t tn, int32_t wk, int3
  * a wider matrix may be given).  codes, scales, packed weights, caches and workspaces: 16-byte aligned.
  * These calls allocate nothing and do not synchronise, so they can be captured into a graph.  A
  * workspace holds nothing between calls; calls (and captured graphs) that may run at the same time need
- * one each.                                                                                        */
+ * one each.  SJD_EINVAL: a size, type, alignment or workspace that does not fit, or a launch of 2^32 threads
+ * (hundreds of millions of rows).                                                                   */
 #define SJD_MX8 8                  /* E4M3 */
 #define SJD_MX4 4                  /* E2M1 */
 #define SJD_MX_MAX_K (1 << 20)     /* longest row */
@@ -391,7 +392,7 @@ int sjd_kv8_append(int32_t dtype, const void *k, const void *v, int64_t ld, cons
  * included: softmax(q k / sqrt(head_dim)) v.  The query at position p sees the positions j <= p with, if window > 0, also
  * j > p - window or j < sinks.  Query head h reads cache head h / (n_heads / n_kv_heads).  out dev, like q, rows of length ldo,
  * of the same dtype (which also says how finely probabilities are held: 22 bits for fp32, 11 for bf16).  workspace:
- * sjd_kv8_attention_workspace bytes.  What masked positions hold, NaN included, does not reach `out`.               */
+ * sjd_kv8_attention_workspace bytes (may be 0).  n_seqs is at most 32767, n_seqs * ceil(L * n_heads / n_kv_heads / 16) at most 65535.  What masked positions hold, NaN included, does not reach `out`.               */
 int sjd_kv8_attention_workspace(int32_t n_seqs, int32_t L, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t cap,
                                 size_t *bytes);
 int sjd_kv8_attention(int32_t dtype, const void *q, int64_t ldq, const uint8_t *cache, const uint8_t *scales, const int32_t *len,

@@ -6,7 +6,6 @@
 #include "sjd_mx.h"
 
 #include <algorithm>
-#include <type_traits>
 
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;

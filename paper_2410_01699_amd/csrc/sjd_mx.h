@@ -75,6 +75,8 @@ template <> __device__ __forceinline__ void mx_load8<bf16_t>(const bf16_t *row, 
 }
 // Whether rows of `ld` elements from p on start at multiples of 16 bytes
 static inline bool mx_vec(const void *p, int64_t ld, int dtype) { return (uintptr_t)p % 16 == 0 && ld * (dtype ? 2 : 4) % 16 == 0; }
+// (what a launch holds: fewer than 2^32 threads in its first dimension)
+static inline bool mx_fits(int64_t workgroups, int threads) { return workgroups * threads < (int64_t)1 << 32; }
 static inline bool mx_aligned(const void *p) { return (uintptr_t)p % 16 == 0; }
 
 // A block of 32 values lies in the 4 lanes of a quad, eight each: its scale byte, the same in all four.  bad: a value of the

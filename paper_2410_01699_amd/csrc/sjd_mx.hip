@@ -42,7 +42,9 @@ extern "C" int sjd_mx_quantize(int32_t format, int32_t dtype, const void *x, con
     const int Kp = mx_up(K, 128);
     int tx = 16;
     while (tx < 256 && tx * 8 < Kp) tx *= 2;
-    const dim3 grid((unsigned)(((int64_t)rows + 256 / tx - 1) / (256 / tx)), (unsigned)((Kp / 8 + tx - 1) / tx));
+    const int64_t groups = ((int64_t)rows + 256 / tx - 1) / (256 / tx);
+    if (!mx_fits(groups, 256)) return SJD_EINVAL;
+    const dim3 grid((unsigned)groups, (unsigned)((Kp / 8 + tx - 1) / tx));
     const int vec = mx_vec(x, ld, dtype) && (!up || mx_vec(up, ld, dtype));
     hipStream_t s = (hipStream_t)stream;
 #define GO(T, F, G) SJD_LAUNCH((mx_quantize_kernel<T, F, G>), grid, dim3(256), 0, s, (const T *)x, (const T *)up, ld, rows, K, Kp, tx, vec, codes, scales)
@@ -139,6 +141,7 @@ extern "C" int sjd_mx_rmsnorm(int32_t format, int32_t dtype, const void *x, int6
     if (!mx_aligned(codes) || !mx_aligned(scales)) return SJD_EINVAL;
     const int dp = mx_up(d, 128);
     const int threads = std::min(1024, mx_up(dp / 8, 64));
+    if (!mx_fits(rows, threads)) return SJD_EINVAL;
     const int vx = x && mx_vec(x, ldx, dtype), vr = resid && mx_vec(resid, ldr, 0), vg = mx_aligned(gain);
     hipStream_t s = (hipStream_t)stream;
 #define GO(T, F) SJD_LAUNCH((mx_rmsnorm_kernel<T, F>), dim3(rows), dim3(threads), 0, s, (const T *)x, ldx, resid, ldr, gain, eps, d, dp, vx, vr, vg, codes, scales)
@@ -195,7 +198,7 @@ extern "C" int sjd_mx_weights(int32_t dtype, const void *W, int64_t ld, int32_t 
 {
     if (!W || !packed || N < 1 || K < 1 || K > SJD_MX_MAX_K || ld < K || (dtype != 0 && dtype != 1) || !mx_aligned(packed)) return SJD_EINVAL;
     const int64_t grid = (((int64_t)N + 15) / 16) * mx_groups(K);
-    if (grid > INT32_MAX) return SJD_EINVAL;
+    if (!mx_fits(grid, 256)) return SJD_EINVAL;
     const int vec = mx_vec(W, ld, dtype);
     hipStream_t s = (hipStream_t)stream;
     if (dtype == 0) SJD_LAUNCH((mx_weights_kernel<float>), dim3((unsigned)grid), dim3(256), 0, s, (const float *)W, ld, N, K, mx_groups(K), vec, packed);

@@ -381,6 +381,7 @@ extern "C" int sjd_mx_product(int32_t format, const uint8_t *codes, const uint8_
     if (need && (!workspace || workspace_bytes < need || !mx_aligned(workspace))) return SJD_EINVAL;
     const int Kp = mx_up(K, 128), tiles = (int)(((int64_t)N + 15) / 16), groups = mx_groups(K);
     const MxPlan p = mx_plan(M, N, K);
+    if (!mx_fits(p.kind < 0 ? ((int64_t)tiles + p.tn - 1) / p.tn : p.wgs, 512)) return SJD_EINVAL;
     const int vec = (uintptr_t)C % (dtype ? 8 : 16) == 0 && ldc % 4 == 0;
     hipStream_t s = (hipStream_t)stream;
     float *part = (float *)workspace;

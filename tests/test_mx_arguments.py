@@ -29,12 +29,13 @@ ATTEND = dict(dtype=0, q=P, ldq=256, cache=P, scales=P, len=P, n_seqs=2, L=4, he
 
 REFUSED = [
     ("sjd_mx_quantize", QUANT, [dict(format=6), dict(dtype=2), dict(dtype=-1), dict(x=None), dict(codes=None), dict(scales=None), dict(ld=63), dict(rows=0),
-                                dict(K=0), dict(K=B.SJD_MX_MAX_K + 1, ld=1 << 40), dict(codes=ODD), dict(scales=ODD)]),
+                                dict(K=0), dict(K=B.SJD_MX_MAX_K + 1, ld=1 << 40), dict(codes=ODD), dict(scales=ODD),
+                                dict(rows=2 ** 31 - 1)]),
     ("sjd_mx_rmsnorm", NORM, [dict(format=0), dict(dtype=2), dict(x=None, resid=None), dict(gain=None), dict(codes=None), dict(scales=None), dict(ldx=63),
-                              dict(ldr=63), dict(rows=0), dict(rows=-1), dict(d=0), dict(eps=-1.0), dict(eps=float("nan")), dict(codes=ODD), dict(scales=ODD)]),
-    ("sjd_mx_weights", WEIGHTS, [dict(dtype=2), dict(W=None), dict(packed=None), dict(packed=ODD), dict(ld=63), dict(N=0), dict(K=0)]),
+                              dict(ldr=63), dict(rows=0), dict(rows=-1), dict(d=0), dict(eps=-1.0), dict(eps=float("nan")), dict(codes=ODD), dict(scales=ODD), dict(rows=2 ** 31 - 1)]),
+    ("sjd_mx_weights", WEIGHTS, [dict(dtype=2), dict(W=None), dict(packed=None), dict(packed=ODD), dict(ld=63), dict(N=0), dict(K=0), dict(N=2 ** 31 - 1)]),
     ("sjd_mx_product", PRODUCT, [dict(format=5), dict(dtype=2), dict(codes=None), dict(scales=None), dict(packed=None), dict(C=None), dict(M=0), dict(N=0),
-                                 dict(K=0), dict(ldc=15), dict(codes=ODD), dict(scales=ODD), dict(packed=ODD)]),
+                                 dict(K=0), dict(ldc=15), dict(N=2 ** 31 - 1, ldc=2 ** 31), dict(codes=ODD), dict(scales=ODD), dict(packed=ODD)]),
     ("sjd_kv8_append", APPEND, [dict(dtype=2), dict(k=None), dict(v=None), dict(len=None), dict(cache=None), dict(scales=None), dict(cache=ODD), dict(scales=ODD),
                                 dict(ld=127), dict(n_seqs=0), dict(n_seqs=1 << 20), dict(L=0), dict(L=65), dict(n_kv=0), dict(n_kv=1 << 20, ld=1 << 40), dict(hd=48),
                                 dict(hd=0), dict(hd=512, ld=2048), dict(cap=0), dict(cap=2 ** 31 - 1)]),
