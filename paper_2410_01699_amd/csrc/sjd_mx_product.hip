@@ -314,23 +314,28 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const float *__restrict__ 
 }
 
 // ---- which kernel ---------------------------------------------------------------------------
-// Whichever is estimated to be done first.  A launch takes as long as its weights from memory or as the CU with most workgroups: so many
-// steps (records) times what one costs, measured with K = 4096 and cold weights in us, bf16 results, activations in 8 bits:
-//  - tiles, a step of a workgroup alone on its CU and of one among several (below);
-//  - few rows, 0.6 + (records / 8) (1.5 + 0.6 TN) for 16 rows, (3.4 + 0.6 TN) for 32; several workgroups of
-//    16 rows on a CU take a seventh less.
-// Slices of K add their sums' way through memory and a launch.  us, measured, the kernel chosen and the next best ones:
+// Whichever is estimated to be done first.  A launch takes as long as its weights from memory or as the CU with most workgroups: something
+// fixed and so many steps (records) times what one costs, fitted to measured times with cold weights in us, bf16 results, activations in 8 bits
+// (within 5 % for most of 53 shapes of 100 to 2048 rows, K from 1536 to 11008):
+//  - tiles: where a CU has one workgroup, and where it has several (below);
+//  - few rows: 0.6 + (records / 8) (1.5 + 0.6 TN) for 16 rows, several workgroups on a CU a seventh less; for 32 rows 2 + 0.4 a workgroup +
+//    (records / 8) (2.6 + 0.95 TN).
+// Slices of K add their sums' way through memory and a launch.  What this takes is 0.7 % slower than the best of all over those shapes, 12 %
+// at most.  us, measured, the kernel chosen and the next best ones:
 //   16 rows    22016 x 4096   rows 6 tiles 11.1   3 tiles 11.7, 1 tile 17.0           (weights alone 7.5)
-//   64         4096 x 4096    rows 2 tiles 7.7    rows 4 tiles 9.0, 64 x 64 in 4 slices 10.0
-//   64         22016 x 4096   64 x 128 18.5       64 x 64 20.2, rows 4 tiles 26.9
-//   128        22016 x 4096   64 x 192 21.3       128 x 128 25.0, 64 x 128 26.1
-//   128        4096 x 11008   64 x 128 in 4 slices 17.0   rows 4 tiles 18.5, in 2 slices 23.0
-//   512        4096 x 4096    64 x 128 16.9       128 x 128 23.7, 128 x 192 33.1
-//   2048       22016 x 4096   256 x 256 178       128 x 192 181, 128 x 128 201
-//   2048       4096 x 4096    128 x 256 36.8      128 x 128 39.0, 256 x 256 59.7
-struct MxTile { int bm, bn; double alone, among; };
-static const MxTile mx_tiles[] = {{64, 64, 0.375, 0.26}, {64, 128, 0.45, 0.33}, {64, 192, 0.59, 0.45}, {128, 128, 0.70, 0.57},
-                                  {128, 192, 0.98, 0.78}, {128, 256, 1.07, 1.07}, {256, 256, 1.80, 1.80}};
+//   100        4096 x 4096    rows 4 tiles 8.4    64 x 64 in 2 slices 12.2, 64 x 64 14.2
+//   100        8192 x 1536    64 x 64 7.7         rows 4 tiles 9.0, 64 x 128 9.1
+//   100        4096 x 11008   64 x 128 in 4 slices 16.9   rows 4 tiles 17.0, in 2 slices 22.8
+//   200        4096 x 4096    64 x 64 14.0        64 x 128 in 2 slices 14.9, rows 4 tiles 15.5
+//   256        12288 x 4096   64 x 192 20.8       64 x 128 24.7, 128 x 128 25.0
+//   512        4096 x 4096    64 x 128 17.0       64 x 64 18.0, 128 x 128 23.6
+//   1024       8192 x 1536    128 x 256 19.2      128 x 128 20.4, 64 x 192 20.6
+//   2048       12288 x 4096   128 x 192 97.6      128 x 256 107, 128 x 128 112
+//   2048       22016 x 4096   256 x 256 177       128 x 192 180, 128 x 128 194
+struct MxTile { int bm, bn; struct { double fixed, step; } one, several; };
+static const MxTile mx_tiles[] = {{64, 64, {3.4, 0.33}, {3.4, 0.226}}, {64, 128, {4.7, 0.364}, {4.5, 0.307}}, {64, 192, {5.9, 0.41}, {5.7, 0.38}},
+                                  {128, 128, {7.1, 0.517}, {7.9, 0.51}}, {128, 192, {8.4, 0.77}, {9.5, 0.633}}, {128, 256, {7.8, 0.864}, {13.9, 0.933}},
+                                  {256, 256, {12.3, 1.46}, {1.7, 1.82}}};
 struct MxPlan { int kind, tn, mt, slices, per, wgs; };      // kind: -1 few rows, else the tile
 static MxPlan mx_plan(int M, int N, int K)
 {
@@ -343,7 +348,8 @@ static MxPlan mx_plan(int M, int N, int K)
     for (int tn : {1, 2, 3, 4, 6}) {
         if ((mt == 2 && tn == 6) || M > 32 * 65535) continue;          // (what a grid holds)
         const double wgs = std::ceil(tiles / tn) * std::ceil(M / (16.0 * mt)), n = std::ceil(wgs / 256);
-        const double t = n * (0.6 + std::max(groups / 8.0, 0.4) * ((mt == 1 ? 1.5 : 3.4) + 0.6 * tn)) * (n > 1 && mt == 1 ? 0.85 : 1);
+        const double records = std::max(groups / 8.0, 0.4);
+        const double t = mt == 1 ? n * (0.6 + records * (1.5 + 0.6 * tn)) * (n > 1 ? 0.85 : 1) : 2 + n * (0.4 + records * (2.6 + 0.95 * tn));
         // (where memory bounds both: the one with less beside it)
         take(std::max(t, stream) + 0.01 * t, {-1, tn, mt, 1, 0, 0});
     }
@@ -354,8 +360,8 @@ static MxPlan mx_plan(int M, int N, int K)
             if (wgs > INT32_MAX) continue;
             for (int sl = 1; sl <= 4 && (sl == 1 || steps >= 8 * sl); sl *= 2) {
                 const int per = mx_up((steps + sl - 1) / sl, 4), slices = (steps + per - 1) / per;
-                const double n = std::ceil((double)wgs * slices / 256), t = per * (n > 1 ? n * x.among : x.alone);
-                const double join = slices > 1 ? 2.5 + (double)M * N * 4 * (slices + 1) / 5e6 : 0;
+                const double n = std::ceil((double)wgs * slices / 256), t = n > 1 ? x.several.fixed + per * n * x.several.step : x.one.fixed + per * x.one.step;
+                const double join = slices > 1 ? 1 + 1.6e-6 * M * N * slices : 0;
                 take(std::max(t, stream) + 0.01 * t + join, {k, 0, 0, slices, per, (int)wgs});
             }
         }
