@@ -373,6 +373,17 @@ int sjd_mx_product_workspace(int32_t M, int32_t N, int32_t K, size_t *bytes);
 int sjd_mx_product(int32_t format, const uint8_t *codes, const uint8_t *scales, const uint8_t *packed, int32_t M, int32_t N,
                    int32_t K, int32_t dtype, void *C, int64_t ldc, void *workspace, size_t workspace_bytes, void *stream);
 
+/* Which kernel sjd_mx_product runs on (no GPU needed): *rows x *cols of C to a workgroup, K in *slices.  16 or 32 rows: the kernel for
+ * few rows, whose waves split K; else one of 64 x 64, 64 x 128, 64 x 192, 128 x 128, 128 x 192, 128 x 256 and 256 x 256, for more than
+ * 32 rows, in 1, 2 or 4 slices (of whole groups of 512 values, so perhaps fewer).                     */
+int sjd_mx_product_plan(int32_t M, int32_t N, int32_t K, int32_t *rows, int32_t *cols, int32_t *slices);
+
+/* sjd_mx_product on the kernel that is named as above, whatever the plan says; workspace: slices * M * (N up to a multiple of 4) floats
+ * where slices > 1.  For kernel-level parity tests.  SJD_EINVAL for a kernel that no plan has for M.     */
+int sjd_mx_product_test(int32_t rows, int32_t cols, int32_t slices, int32_t format, const uint8_t *codes, const uint8_t *scales,
+                        const uint8_t *packed, int32_t M, int32_t N, int32_t K, int32_t dtype, void *C, int64_t ldc, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
 /* A cache in 8 bits of n_seqs sequences, `cap` positions each: cache dev [n_seqs][n_kv_heads][ceil(cap / 32)][64 * head_dim],
  * scales dev [n_seqs][n_kv_heads][ceil(cap / 32)][2] (keys, values).  head_dim: 32, 64, 96, 128 or 256.  A block's record
  * holds its keys, then its values, as the lanes of the attention read them:

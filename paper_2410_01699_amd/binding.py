@@ -30,6 +30,7 @@ EXPORTS = ["sjd_init_model", "sjd_free_model", "sjd_kv_create", "sjd_kv_free", "
            "sjd_prefill_uncond", "sjd_generate_cfg", "sjd_decode_steps_batch", "sjd_forward_logits_batch",
            "sjd_generate_batch", "sjd_profile_steps_batch", "sjd_verify_static", "sjd_gemm_plan",
            "sjd_mx_quantize", "sjd_mx_rmsnorm", "sjd_mx_weights_bytes", "sjd_mx_weights", "sjd_mx_product_workspace", "sjd_mx_product",
+           "sjd_mx_product_plan", "sjd_mx_product_test",
            "sjd_kv8_append", "sjd_kv8_attention_workspace", "sjd_kv8_attention"]
 
 PROF_KINDS = ("gemm", "attention", "elementwise", "verify")
@@ -117,6 +118,8 @@ _SIG = {
     "sjd_mx_weights": (C.c_int, [_i32, _vp, _i64, _i32, _i32, _vp, _vp]),
     "sjd_mx_product_workspace": (C.c_int, [_i32, _i32, _i32, _P(_sz)]),
     "sjd_mx_product": (C.c_int, [_i32, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _sz, _vp]),
+    "sjd_mx_product_plan": (C.c_int, [_i32, _i32, _i32, _P(_i32), _P(_i32), _P(_i32)]),
+    "sjd_mx_product_test": (C.c_int, [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _sz, _vp]),
     "sjd_kv8_append": (C.c_int, [_i32, _vp, _vp, _i64, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp]),
     "sjd_kv8_attention_workspace": (C.c_int, [_i32, _i32, _i32, _i32, _i32, _i32, _P(_sz)]),
     "sjd_kv8_attention": (C.c_int, [_i32, _vp, _i64, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _sz,
@@ -491,6 +494,24 @@ def sjd_mx_product(format, codes, scales, packed, K, out, workspace, stream=None
     pw = _flat(dev, "packed", packed, sjd_mx_weights_bytes(N, K))
     ws, ws_bytes = _workspace(dev, workspace, sjd_mx_product_workspace(M, N, K))
     _done(_lib.sjd_mx_product(format, pc, ps, pw, M, N, K, dt, po, ld, ws, ws_bytes, _on(stream)))
+
+
+def sjd_mx_product_plan(M, N, K):
+    """(rows, columns of a workgroup, K-slices) of the kernel that a product runs on; needs no GPU"""
+    r = [_i32(0) for _ in range(3)]
+    _check(_lib.sjd_mx_product_plan(M, N, K, *[C.byref(x) for x in r]))
+    return tuple(x.value for x in r)
+
+
+def sjd_mx_product_test(plan, format, codes, scales, packed, K, out, workspace, stream=None):
+    """sjd_mx_product on the kernel `plan` (as sjd_mx_product_plan gives it)"""
+    dev = _device(out)
+    M, N = _matrix("out", out)
+    po, dt, ld = _rows(dev, "out", out, M, N)
+    pc, ps = _coded(dev, format, M, K, codes, scales)
+    pw = _flat(dev, "packed", packed, sjd_mx_weights_bytes(N, K))
+    ws, ws_bytes = _workspace(dev, workspace, plan[2] * M * ((N + 3) // 4 * 4) * 4 if plan[2] > 1 else 0)
+    _done(_lib.sjd_mx_product_test(*plan, format, pc, ps, pw, M, N, K, dt, po, ld, ws, ws_bytes, _on(stream)))
 
 
 def _kv8(dev, cache, scales, n_seqs, n_kv, hd, cap):

@@ -368,25 +368,27 @@ static MxPlan mx_plan(int M, int N, int K)
     return best;
 }
 
-extern "C" int sjd_mx_product_workspace(int32_t M, int32_t N, int32_t K, size_t *bytes)
-{
-    if (!bytes || M < 1 || N < 1 || K < 1 || K > SJD_MX_MAX_K) return SJD_EINVAL;
-    const MxPlan p = mx_plan(M, N, K);
-    *bytes = p.slices > 1 ? (size_t)p.slices * M * mx_up(N, 4) * sizeof(float) : 0;
-    return SJD_OK;
-}
-
-extern "C" int sjd_mx_product(int32_t format, const uint8_t *codes, const uint8_t *scales, const uint8_t *packed, int32_t M, int32_t N,
-                              int32_t K, int32_t dtype, void *C, int64_t ldc, void *workspace, size_t workspace_bytes, void *stream)
+static int mx_product_args(int32_t format, const uint8_t *codes, const uint8_t *scales, const uint8_t *packed, int32_t M, int32_t N, int32_t K,
+                           int32_t dtype, void *C, int64_t ldc)
 {
     if (!codes || !scales || !packed || !C || M < 1 || N < 1 || K < 1 || K > SJD_MX_MAX_K || ldc < N) return SJD_EINVAL;
     if ((format != SJD_MX8 && format != SJD_MX4) || (dtype != 0 && dtype != 1)) return SJD_EINVAL;
-    if (!mx_aligned(codes) || !mx_aligned(scales) || !mx_aligned(packed)) return SJD_EINVAL;
-    size_t need = 0;
-    SJD_TRY(sjd_mx_product_workspace(M, N, K, &need));
-    if (need && (!workspace || workspace_bytes < need || !mx_aligned(workspace))) return SJD_EINVAL;
+    return mx_aligned(codes) && mx_aligned(scales) && mx_aligned(packed) ? SJD_OK : SJD_EINVAL;
+}
+static size_t mx_product_bytes(const MxPlan &p, int M, int N) { return p.slices > 1 ? (size_t)p.slices * M * mx_up(N, 4) * sizeof(float) : 0; }
+
+extern "C" int sjd_mx_product_workspace(int32_t M, int32_t N, int32_t K, size_t *bytes)
+{
+    if (!bytes || M < 1 || N < 1 || K < 1 || K > SJD_MX_MAX_K) return SJD_EINVAL;
+    *bytes = mx_product_bytes(mx_plan(M, N, K), M, N);
+    return SJD_OK;
+}
+
+// The sums of C on the kernel that `p` names; arguments are checked
+static int mx_product_on(const MxPlan &p, int32_t format, const uint8_t *codes, const uint8_t *scales, const uint8_t *packed, int M, int N, int K,
+                         int32_t dtype, void *C, int64_t ldc, void *workspace, void *stream)
+{
     const int Kp = mx_up(K, 128), tiles = (int)(((int64_t)N + 15) / 16), groups = mx_groups(K);
-    const MxPlan p = mx_plan(M, N, K);
     if (!mx_fits(p.kind < 0 ? ((int64_t)tiles + p.tn - 1) / p.tn : p.wgs, 512)) return SJD_EINVAL;
     const int vec = (uintptr_t)C % (dtype ? 8 : 16) == 0 && ldc % 4 == 0;
     hipStream_t s = (hipStream_t)stream;
@@ -420,4 +422,49 @@ extern "C" int sjd_mx_product(int32_t format, const uint8_t *codes, const uint8_
         HIP_TRY(hipGetLastError());
     }
     return SJD_OK;
+}
+
+extern "C" int sjd_mx_product(int32_t format, const uint8_t *codes, const uint8_t *scales, const uint8_t *packed, int32_t M, int32_t N,
+                              int32_t K, int32_t dtype, void *C, int64_t ldc, void *workspace, size_t workspace_bytes, void *stream)
+{
+    SJD_TRY(mx_product_args(format, codes, scales, packed, M, N, K, dtype, C, ldc));
+    const MxPlan p = mx_plan(M, N, K);
+    const size_t need = mx_product_bytes(p, M, N);
+    if (need && (!workspace || workspace_bytes < need || !mx_aligned(workspace))) return SJD_EINVAL;
+    return mx_product_on(p, format, codes, scales, packed, M, N, K, dtype, C, ldc, workspace, stream);
+}
+
+extern "C" int sjd_mx_product_plan(int32_t M, int32_t N, int32_t K, int32_t *rows, int32_t *cols, int32_t *slices)
+{
+    if (!rows || !cols || !slices || M < 1 || N < 1 || K < 1 || K > SJD_MX_MAX_K) return SJD_EINVAL;
+    const MxPlan p = mx_plan(M, N, K);
+    *rows = p.kind < 0 ? 16 * p.mt : mx_tiles[p.kind].bm;
+    *cols = p.kind < 0 ? 16 * p.tn : mx_tiles[p.kind].bn;
+    *slices = p.slices;
+    return SJD_OK;
+}
+
+extern "C" int sjd_mx_product_test(int32_t rows, int32_t cols, int32_t slices, int32_t format, const uint8_t *codes, const uint8_t *scales,
+                                   const uint8_t *packed, int32_t M, int32_t N, int32_t K, int32_t dtype, void *C, int64_t ldc, void *workspace,
+                                   size_t workspace_bytes, void *stream)
+{
+    SJD_TRY(mx_product_args(format, codes, scales, packed, M, N, K, dtype, C, ldc));
+    MxPlan p = {-2, 0, 0, 1, 0, 0};
+    if (rows <= 32) {
+        const int tn = cols / 16;
+        if ((rows != 16 && rows != 32) || cols != 16 * tn || tn < 1 || tn > (rows == 16 ? 6 : 4) || tn == 5 || slices != 1 || M > 32 * 65535) return SJD_EINVAL;
+        if ((rows == 16) != (M <= 16)) return SJD_EINVAL;      // (as the plan has it)
+        p = {-1, tn, rows / 16, 1, 0, 0};
+    }
+    for (int k = 0; k < 7; ++k) {
+        if (mx_tiles[k].bm != rows || mx_tiles[k].bn != cols || M <= 32 || (slices != 1 && slices != 2 && slices != 4)) continue;
+        const int64_t wgs = (((int64_t)M + rows - 1) / rows) * (((int64_t)N + cols - 1) / cols);
+        if (wgs > INT32_MAX) return SJD_EINVAL;
+        const int steps = mx_up(K, 128) / 128, per = mx_up((steps + slices - 1) / slices, 4);
+        p = {k, 0, 0, (steps + per - 1) / per, per, (int)wgs};
+    }
+    if (p.kind == -2) return SJD_EINVAL;
+    const size_t need = mx_product_bytes(p, M, N);
+    if (need && (!workspace || workspace_bytes < need || !mx_aligned(workspace))) return SJD_EINVAL;
+    return mx_product_on(p, format, codes, scales, packed, M, N, K, dtype, C, ldc, workspace, stream);
 }

@@ -1,0 +1,76 @@
+"""The 4-bit product on each of its kernels (GPU only), whatever the plan would take at these sizes."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from test_gpu_mx import B, TYPES, check_product, operands  # noqa: E402,F401
+
+pytestmark = pytest.mark.gpu
+
+TILES = [(64, 64), (64, 128), (64, 192), (128, 128), (128, 192), (128, 256), (256, 256)]
+ROWS = [(16, 16 * t) for t in (1, 2, 3, 4, 6)] + [(32, 16 * t) for t in (1, 2, 3, 4)]
+# K of 1 to 9 steps of 128 values and a few more: the loop of four and what is left of it, records that end after 1 to 4 steps, rows
+# that end inside a step
+LENGTHS = [70, 256, 300, 512, 600, 768, 900, 1024, 1100, 1536, 1900]
+
+
+def run(B, plan, gpu, M, N, K, bits, dtype, out=None):
+    out = torch.full((M, N), float("nan"), dtype=TYPES[dtype], device="cuda") if out is None else out
+    ws = torch.full((plan[2] * M * ((N + 3) // 4 * 4) * 4,), 0xFF, dtype=torch.uint8, device="cuda") if plan[2] > 1 else None
+    B.sjd_mx_product_test(plan, bits, *gpu, K, out, ws)
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("rows,cols", ROWS + TILES, ids=lambda v: str(v))
+def test_every_kernel(B, rows, cols, bits, dtype):
+    """fewer rows than a workgroup has and one more than two have; features that end inside a tile of 16, inside a wave's tiles, and behind them"""
+    for i, K in enumerate(LENGTHS):
+        M, N = [(rows + 1 if rows > 32 else rows, cols - 3), (2 * rows + 1, cols + 17), (max(rows - 31, 33), 2 * cols + 50), (rows + 16, 31)][i % 4]
+        M = max(1, rows - i) if rows == 16 else M
+        gpu, a, w = operands(M, N, K, bits, seed=30 + i)
+        check_product(run(B, (rows, cols, 1), gpu, M, N, K, bits, dtype), a, w, K, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("rows,cols", TILES, ids=lambda v: str(v))
+def test_every_tile_in_slices(B, rows, cols, bits, dtype):
+    """K in 2 and 4 slices, the last one shorter, joined by the second kernel; rows of odd length, which it writes value by value"""
+    for M, N, K, slices in ((rows + 9, cols + 3, 1100, 2), (77, cols - 1, 2050, 4), (2 * rows, cols + 20, 4096, 2), (70, 50, 5700, 4)):
+        gpu, a, w = operands(M, N, K, bits, seed=50 + slices)
+        check_product(run(B, (rows, cols, slices), gpu, M, N, K, bits, dtype), a, w, K, dtype)
+    wide = torch.full((40, 90), 7.0, dtype=TYPES[dtype], device="cuda")
+    gpu, a, w = operands(40, 83, 1300, bits)
+    check_product(run(B, (rows, cols, 2), gpu, 40, 83, 1300, bits, dtype, wide[:, :83]), a, w, 1300, dtype)
+    assert (wide[:, 83:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("rows,cols", ROWS + TILES, ids=lambda v: str(v))
+def test_nan_stays_in_its_row_and_column_on_every_kernel(B, rows, cols, bits, dtype):
+    M, N = (9 if rows == 16 else rows + 40), 100
+    for K, slices in ((1024, 1), (700, 1)) + (((2100, 2),) if rows > 32 else ()):
+        gpu, a, w = operands(M, N, K, bits)
+        ref = run(B, (rows, cols, slices), gpu, M, N, K, bits, dtype)
+        codes, scales, packed = (t.clone() for t in gpu)
+        if bits == 8:
+            codes[1, 600] = 0x7F
+        else:
+            scales[1, 18] = 255
+        groups = -(-K // 512)
+        packed.view(-1, groups, 4352)[3, 1, 4096 + 4 * (16 * 2 + 5) + 1] = 255       # feature 53, a block of the second 512 values
+        out = run(B, (rows, cols, slices), (codes, scales, packed), M, N, K, bits, dtype)
+        hit = torch.zeros(M, N, dtype=torch.bool, device="cuda")
+        hit[1], hit[:, 53] = True, True
+        assert torch.isnan(out[hit]).all() and torch.equal(out[~hit], ref[~hit])
+
+
+def test_what_the_hook_refuses(B):
+    gpu, a, w = operands(40, 100, 512, 8)
+    for plan in ((48, 64, 1), (64, 65, 1), (64, 256, 1), (64, 64, 3), (64, 64, 0), (64, 64, 8), (16, 16, 1), (32, 96, 1), (32, 16, 2), (32, 80, 1), (32, 0, 1), (0, 0, 1)):
+        with pytest.raises(B.SjdError) as e:
+            run(B, plan, gpu, 40, 100, 512, 8, "fp32")
+        assert e.value.code == B.SJD_EINVAL, plan

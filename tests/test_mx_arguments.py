@@ -102,3 +102,35 @@ def test_packed_orders_hold_every_value_once():
     w = R.pack_weights(codes, scales, 21, 640).reshape(2, 2, 4352)
     n, kk = 19, 513 + 128 + 64 + 3 - 130                     # feature 19, value 578: group 1, step 0, quarter 2, value 2 of it
     assert kk == 578 and w[1, 1, 16 * (16 * 2 + 3) + 1] & 15 == codes[n, kk] and w[1, 1, 4096 + 4 * (16 * 2 + 3)] == scales[n, 18]
+
+
+PLANS = {(16, 16 * t, 1) for t in (1, 2, 3, 4, 6)} | {(32, 16 * t, 1) for t in (1, 2, 3, 4)} | {
+    (*t, s) for t in ((64, 64), (64, 128), (64, 192), (128, 128), (128, 192), (128, 256), (256, 256)) for s in (1, 2, 3, 4)}
+
+
+def test_plans_are_kernels_that_exist():
+    """every plan is one that the parity entry takes, and its workspace is what the plan's slices need"""
+    seen = set()
+    for M in (1, 2, 15, 16, 17, 32, 33, 64, 100, 129, 200, 256, 500, 512, 1000, 1024, 2048, 5000, 100000):
+        for N in (1, 16, 50, 256, 1536, 4096, 4608, 8192, 12288, 16384, 22016):
+            for K in (1, 128, 700, 1536, 4096, 11008, 1 << 17):
+                rows, cols, slices = p = B.sjd_mx_product_plan(M, N, K)
+                assert p in PLANS and (rows == 16) == (M <= 16) and (rows <= 32 or M > 32), (M, N, K, p)
+                assert B.sjd_mx_product_workspace(M, N, K) == (slices * M * (-(-N // 4) * 4) * 4 if slices > 1 else 0)
+                seen.add((rows, cols))
+    assert len(seen) == 16                                    # no kernel that nothing reaches
+    n = C.c_int32()
+    for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, 1, B.SJD_MX_MAX_K + 1)):
+        assert B._lib.sjd_mx_product_plan(*bad, C.byref(n), C.byref(n), C.byref(n)) == BAD
+    assert B._lib.sjd_mx_product_plan(1, 1, 1, None, C.byref(n), C.byref(n)) == BAD
+
+
+HOOK = dict(rows=64, cols=64, slices=1, format=8, codes=P, scales=P, packed=P, M=40, N=16, K=640, dtype=0, C=P, ldc=16, ws=P, ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("change", [dict(format=5), dict(dtype=2), dict(codes=None), dict(C=None), dict(K=0), dict(ldc=15), dict(codes=ODD), dict(rows=48), dict(cols=80),
+                                    dict(cols=256), dict(slices=3), dict(slices=0), dict(rows=16, cols=16), dict(rows=32, cols=96), dict(rows=32, cols=80, M=20),
+                                    dict(rows=32, cols=16, slices=2), dict(rows=32, cols=0), dict(M=32), dict(rows=16, cols=96, M=17), dict(rows=0, cols=0),
+                                    dict(slices=2, ws=None), dict(slices=2, ws_bytes=16), dict(slices=2, ws=ODD)])
+def test_the_parity_entry_refuses(change):
+    assert call("sjd_mx_product_test", HOOK, **change) == BAD
