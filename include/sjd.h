@@ -367,8 +367,9 @@ int sjd_mx_weights_bytes(int32_t N, int32_t K, size_t *bytes);
 int sjd_mx_weights(int32_t dtype, const void *W, int64_t ld, int32_t N, int32_t K, uint8_t *packed, void *stream);
 
 /* C[M x N] (dev, dtype, row length ldc) = A W^T: A codes and scales in `format` as above (K values a row), W packed.  fp32 results:
- * products of codes are exact, sums are fp32.  bf16 results: of eight neighbouring products those below 2^-13 of the largest are cut
- * (5e-6 of a result), sums are fp32 and rounded once.  workspace: sjd_mx_product_workspace bytes (may be 0).   */
+ * products of codes are exact, sums are fp32.  bf16 results from E4M3 rows: among eight neighbouring products (columns 8 i .. 8 i + 7)
+ * each is cut towards zero by less than 2^-13 of the largest one; that is 5e-6 of a result in the 2-norm of random rows, and may be all of a
+ * result whose large products cancel.  Sums are fp32 and rounded once.  workspace: sjd_mx_product_workspace bytes (may be 0).   */
 int sjd_mx_product_workspace(int32_t M, int32_t N, int32_t K, size_t *bytes);
 int sjd_mx_product(int32_t format, const uint8_t *codes, const uint8_t *scales, const uint8_t *packed, int32_t M, int32_t N,
                    int32_t K, int32_t dtype, void *C, int64_t ldc, void *workspace, size_t workspace_bytes, void *stream);

@@ -1,8 +1,10 @@
-"""The 4-bit product on each of its kernels (GPU only), whatever the plan would take at these sizes."""
+"""The 4-bit product on each of its kernels (GPU only), whatever the plan would take at these sizes; and products whose sums fp32 holds exactly."""
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 
+import mx_reference as R  # noqa: E402
 from test_gpu_mx import B, TYPES, check_product, operands  # noqa: E402,F401
 
 pytestmark = pytest.mark.gpu
@@ -66,6 +68,61 @@ def test_nan_stays_in_its_row_and_column_on_every_kernel(B, rows, cols, bits, dt
         hit = torch.zeros(M, N, dtype=torch.bool, device="cuda")
         hit[1], hit[:, 53] = True, True
         assert torch.isnan(out[hit]).all() and torch.equal(out[~hit], ref[~hit])
+
+
+def few_large_ones(M, N, K, seed):
+    """Rows of zeros but for six codes of any magnitude, some of them pairs of the largest with opposite signs, and weights of
+    6 and 0.5: every product is a multiple of 2^-10 and below 2^12, so any order of adding six of them in fp32 is exact."""
+    r = np.random.RandomState(seed)
+    codes = np.zeros((M, -(-K // 128) * 128), np.uint8)
+    for m in range(M):
+        at = r.randint(0, K) // 8 * 8 + r.permutation(8)[:6] if m % 2 else r.permutation(K)[:6]      # six of eight neighbours, or anywhere
+        at = np.minimum(at, K - 1)
+        small = r.randint(1, 0x7E, 6)
+        small[0], small[1] = 0x7E, 0xFE                                # 448 and -448
+        if m % 4 == 1:
+            small[2:] = 0x41                                           # 2.25
+        elif m % 4 == 3:
+            small[2:] = r.choice([0x01, 0x3F, 0x40, 0x41, 0x47], 4)      # 2^-9, 1.875, 2, 2.25, 3.75
+        codes[m, at] = small | (r.randint(0, 2, 6) << 7) * (np.arange(6) > 1)
+    w = r.choice(np.array([1, 7, 9, 15], np.uint8), (N, codes.shape[1]))        # 0.5, 6, -0.5, -6
+    w[:, K:] = 0
+    w[0] = np.where(w[0] & 8, 15, 7) * (np.arange(len(w[0])) < K)
+    return codes, w
+
+
+@pytest.mark.parametrize("rows,cols", ROWS + TILES, ids=lambda v: str(v))
+def test_fp32_results_drop_nothing(B, rows, cols):
+    """small products beside large ones that cancel: equal to the sum in 64 bits, to the bit"""
+    K = 1300
+    M, N = (16 if rows == 16 else 500), 100
+    for seed in range(8 if rows == 16 else 2):
+        ca, cw = few_large_ones(M, N, K, seed)
+        sa, sw = np.full((M, ca.shape[1] // 32), 127, np.uint8), np.full((N, ca.shape[1] // 32), 127, np.uint8)
+        gpu = [torch.from_numpy(x).cuda() for x in (ca, sa, R.pack_weights(cw, sw, N, K))]
+        want = R.values(ca, sa, 8) @ R.values(cw, sw, 4).T
+        assert (want == want.astype(np.float32)).all()
+        got = run(B, (rows, cols, 1), gpu, M, N, K, 8, "fp32").double().cpu().numpy()
+        assert np.array_equal(got, want), (np.count_nonzero(got != want), np.abs(got - want).max())
+
+
+@pytest.mark.parametrize("M,N", [(7, 96), (20, 96), (500, 90)])
+def test_bf16_results_cut_what_is_stated(B, M, N):
+    """among eight neighbours each product loses less than 2^-13 of the largest, towards zero; eights are added in fp32 and the result is rounded once"""
+    K = 1300
+    for seed in range(4):
+        ca, cw = few_large_ones(M, N, K, 10 + seed)
+        sa, sw = np.full((M, ca.shape[1] // 32), 127, np.uint8), np.full((N, ca.shape[1] // 32), 127, np.uint8)
+        gpu = [torch.from_numpy(x).cuda() for x in (ca, sa, R.pack_weights(cw, sw, N, K))]
+        a, w = R.values(ca, sa, 8), R.values(cw, sw, 4)
+        lost = np.zeros((M, N))
+        for k in range(0, a.shape[1], 8):
+            p = np.abs(a[:, None, k:k + 8] * w[None, :, k:k + 8])
+            lost += 2.0 ** -13 * p.max(-1) * np.maximum((p > 0).sum(-1) - 1, 0)
+        plan = B.sjd_mx_product_plan(M, N, K)
+        got, want = run(B, plan, gpu, M, N, K, 8, "bf16").double().cpu().numpy(), a @ w.T
+        room = (lost + K * 2.0 ** -24 * (np.abs(a) @ np.abs(w).T)) * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want)
+        assert (np.abs(got - want) <= room).all(), np.max(np.abs(got - want) / room)
 
 
 def test_what_the_hook_refuses(B):
