@@ -159,9 +159,10 @@ extern "C" int sjd_kv8_append(int32_t dtype, const void *k, const void *v, int64
 // against 6.6 (300 positions, one query, 32 heads), 10.1 against 8.4 (583, 16 queries); longer walks gain from the cut.
 #define KV8_SHORT 32
 #define KV8_SKEW 256     // blocks of a cache whose walks may differ by more than a second launch costs
-#define KV8_NEAR_LIFT 12 // probabilities up to 2^KV8_HEADROOM times 2^12 in fp16: 22 bits of hi + lo hold from 2^-14 on, and 2^-37 below
-#define KV8_HEADROOM 3.f
-#define KV8_LIFT 14      // probabilities times 2^14 in fp16: 22 bits of hi + lo hold from 2^-27 of the largest on
+#define KV8_LIFT 12.f    // a row's reference is its largest score less this: weights up to 2^KV8_TOP in fp16, 22 bits of hi + lo hold from
+#define KV8_TOP 15.f     // 2^-14 on, and 2^-37 of the largest below
+#define KV8_O_LIFT 14.f  // weights times value scales, where those differ: 22 bits hold from 2^-27 of the largest on
+#define KV8_FAR 1048576.f        // references from here on: fp32 has 1/8 between scores
 
 // The queries of one sequence that read one cache head, L * (heads per cache head) rows with a query's heads next to each other, are cut
 // into groups of 16 rows.  A (sequence, group) pair walks the blocks that any of its queries sees, the sinks' first.  Where the pairs are too
@@ -255,7 +256,22 @@ __device__ __forceinline__ float kv8_across(float x)
 }
 __device__ __forceinline__ float kv8_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// record of a split: O[KV8_ROWS][HD] in units of 2^(mo - KV8_LIFT), then m, mo and l of the rows; rows behind the last are not written
+// reference for a largest score: far ones have no room for the lift (it would be rounded to more than fp16 holds)
+__device__ __forceinline__ float kv8_ref(float top) { return top - (fabsf(top) < KV8_FAR ? KV8_LIFT : 0.f); }
+// the exponent by which sums with reference m go down to reference M >= m; sums of nothing (m = -inf) go to zero, or stay NaN
+__device__ __forceinline__ float kv8_down(float m, float M) { return m == -INFINITY ? -INFINITY : m - M; }
+// what a score's product has added: less the reference, and nothing while no score is known
+__device__ __forceinline__ float kv8_shift(float m) { return m == -INFINITY ? 0.f : -m; }
+// log2 of a score's weight, s cs + shift.  Far references are roundings of a product, and s cs itself may be many powers of two beside it: the
+// product is rounded likewise before it is compared.
+__device__ __forceinline__ float kv8_log(float s, float cs, float shift)
+{
+    float p = s * cs;
+    asm("" : "+v"(p));                             // (no fused multiply-add)
+    return fabsf(shift) >= KV8_FAR ? p + shift : fmaf(s, cs, shift);
+}
+
+// record of a split: O[KV8_ROWS][HD], then m, d and l of the rows; rows behind the last are not written
 __host__ __device__ __forceinline__ size_t kv8_record(int hd) { return (size_t)KV8_ROWS * (hd + 3); }
 
 __device__ __forceinline__ void kv8_out(float *p, const f32x4 &v, bool vec)
@@ -272,12 +288,12 @@ __device__ __forceinline__ void kv8_out(bf16_t *p, const f32x4 &v, bool vec)
 
 // Per block of 32 positions, with the scales 2^ek and 2^ev of its keys and values:
 //   S^T[key][row] = K codes . Q (Q scaled per row to 2^13 .. 2^14, hi + lo fp16)        s = S * 2^ek * 2^eq * log2(e) / sqrt(HD)
-//   l = sum 2^(s - m),   O = sum 2^(s + ev - mo + KV8_LIFT) * V codes,   out = O * 2^(mo - KV8_LIFT - m) / l
-// with references m and mo that may be any numbers near the largest s and s + ev: O has one of its own because the blocks' scales differ, so
-// that fp16 holds its largest contributions whatever the scales are.
+//   l = sum 2^(s - m),   O = sum 2^(s + ev - m - d) * V codes,   out = O * 2^d / l
+// with a reference m that may be any number near the largest s, and a whole number d: O has one of its own because the blocks' scales differ, so
+// that fp16 holds its largest contributions whatever the scales are.  d is relative to m, so that neither loses bits to the other.
 // Most walks need less.  While the value scales are within a few powers of two of the wave's first one, the codes take the difference when they
-// become fp16 (exactly: 2^-9 2^-5 .. 448 2^6), O keeps to m, and m stays until a score is 2^KV8_HEADROOM above it: what is left of a block beside
-// its conversions (64 codes a lane) is 8 exponentials, their sum and a comparison.  Against references that follow every block: 38.7 us
+// become fp16 (exactly: 2^-9 2^-5 .. 448 2^6), d is that first scale, and m stays until a score is 2^KV8_TOP above it: what is left of a block
+// beside its conversions (64 codes a lane) is 8 exponentials, their sum and a comparison.  Against references that follow every block: 38.7 us
 // against 43.8 (32 queries x 4 heads a cache head, 16 k positions), 15.2 against 16.3 (8 x 16 queries of 32 heads), 19.9 against 22.2
 // (128 queries, 4 k positions); no difference where memory bounds, one query.
 // The two score tiles of a block leave lane (g, c) with row c and the positions 16 h + 4 g + i: the order in which V's operands hold them.
@@ -289,7 +305,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
     constexpr int KS = HD / 32, DT = HD / 16, RG = KV8_ROWS, PL = sizeof(T) == 4 ? 2 : 1, CH = DT < 8 ? DT : 8;
     __shared__ f16x8 q_lds[KS][PL][64];
     __shared__ float q_scale[RG];
-    __shared__ float m_all[KV8_WAVES][RG], mo_all[KV8_WAVES][RG], l_all[KV8_WAVES][RG];
+    __shared__ float m_all[KV8_WAVES][RG], d_all[KV8_WAVES][RG], l_all[KV8_WAVES][RG];
     __shared__ f32x4 o_slot[KV8_WAVES][CH][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
     const int head = blockIdx.x, heads = gridDim.x;
@@ -362,7 +378,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
     f32x4 o[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, mo, l = 0.f;
+    float m = -INFINITY, d, l = 0.f;
     const float qs = q_scale[c];
     const int pos = sp.n + kv8_query(pl, min(r0 + c, rows - 1));
     // S = K codes . Q, then the next block's keys are requested; whole: no row's mask hides anything of the block
@@ -426,14 +442,15 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
     // ---- value scales near the first one ----
     sb = __builtin_amdgcn_readfirstlane(sc);
     const int base = sb >> 8;
-    float shift = KV8_NEAR_LIFT;                 // KV8_NEAR_LIFT - m, or without m while nothing is seen
+    float shift = 0.f;
+    bool far = false;                            // any row of the wave has a far reference
     for (; v < v_end; v += KV8_WAVES) {
         sb = __builtin_amdgcn_readfirstlane(sc);
         const int up = (sb >> 8) - base;
         if (up < -5 || up > 6) break;
         scores();
         const float cs = qs * mx_pow2(sb & 255);
-        float x[8], bm;
+        float bm;
         uint32_t seen = 0xFFu;
         if (whole) {
             bm = s[0][0];
@@ -447,24 +464,25 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
             for (int e = 0; e < 8; ++e) {
                 const bool see = sees(e);
                 seen |= see ? 1u << e : 0u;
-                x[e] = see ? s[e >> 2][e & 3] * cs : -INFINITY;
-                bm = fmaxf(bm, x[e]);
+                bm = fmaxf(bm, see ? s[e >> 2][e & 3] * cs : -INFINITY);
             }
         }
-        if (__ballot(bm > m + KV8_HEADROOM)) {
-            const float mn = fmaxf(m, kv8_across(bm)), turn = mn == -INFINITY ? 1.f : kv8_exp2(m - mn);
+        if (__ballot(bm - m > KV8_TOP)) {
+            const float mn = fmaxf(m, kv8_ref(kv8_across(bm))), turn = mn == -INFINITY ? 1.f : kv8_exp2(kv8_down(m, mn));
             l *= turn;
 #pragma unroll
             for (int t = 0; t < DT; ++t) o[t] *= turn;
             m = mn;
-            shift = mn == -INFINITY ? KV8_NEAR_LIFT : KV8_NEAR_LIFT - mn;
+            shift = kv8_shift(m);
+            far = __ballot(fabsf(shift) >= KV8_FAR) != 0;
         }
-        if (whole) {
+        float x[8];
+        if (whole && !far) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = kv8_exp2(fmaf(s[e >> 2][e & 3], cs, shift));
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = kv8_exp2(x[e] + shift);
+            for (int e = 0; e < 8; ++e) x[e] = seen >> e & 1 ? kv8_exp2(kv8_log(s[e >> 2][e & 3], cs, shift)) : 0.f;
         }
         f16x8 ph, plo = {};
 #pragma unroll
@@ -475,40 +493,41 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
         }
         weigh(ph, plo, seen, mx_pow2(127 + up));
     }
-    l *= mx_pow2(127 - KV8_NEAR_LIFT);
-    mo = m + (float)(base - 127 + KV8_LIFT - KV8_NEAR_LIFT);
+    d = (float)(base - 127);
     // ---- the rest of a walk whose value scales differ by more ----
     for (; v < v_end; v += KV8_WAVES) {
         sb = __builtin_amdgcn_readfirstlane(sc);
         scores();
         const float cs = qs * mx_pow2(sb & 255), ev = (float)((sb >> 8) - 127);
-        float x[8], bm = -INFINITY;
+        float bm = -INFINITY;
         uint32_t seen = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const bool see = whole || sees(e);
             seen |= see ? 1u << e : 0u;
-            x[e] = see ? s[e >> 2][e & 3] * cs : -INFINITY;
-            bm = fmaxf(bm, x[e]);
+            bm = fmaxf(bm, see ? s[e >> 2][e & 3] * cs : -INFINITY);
         }
         bm = kv8_across(bm);
-        const float mn = fmaxf(m, bm), mon = fmaxf(mo, bm + ev);
-        const float so = mn == -INFINITY ? 1.f : kv8_exp2(m - mn);
-        const float f = mn == -INFINITY ? 0.f : kv8_exp2(fminf(ev - mon + mn + KV8_LIFT, 120.f));
-        const float turn = mon == -INFINITY ? 1.f : kv8_exp2(mo - mon);      // what the output so far is rescaled by
+        const float mn = fmaxf(m, kv8_ref(bm));
+        const bool none = mn == -INFINITY;                                   // nothing seen so far
+        const float down = none ? 0.f : kv8_down(m, mn);
+        const float dn = none ? d : rintf(fmaxf(d + down, kv8_down(bm, mn) + ev - KV8_O_LIFT));
+        const float so = kv8_exp2(down), turn = kv8_exp2(down + (d - dn));      // what the sums so far are rescaled by
+        const float f = none ? 0.f : kv8_exp2(fminf(ev - dn, 120.f));
+        shift = kv8_shift(mn);
         float sum = 0.f;
         f16x8 ph, plo = {};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            x[e] = seen >> e & 1 ? kv8_exp2(x[e] - mn) : 0.f;
-            sum += x[e];
-            float pf = x[e] * f;
+            const float x = seen >> e & 1 ? kv8_exp2(kv8_log(s[e >> 2][e & 3], cs, shift)) : 0.f;
+            sum += x;
+            float pf = x * f;
             if (PL == 2) asm("" : "+v"(pf));     // (the product in fp32 for both parts: fused into the conversion to fp16 it rounds otherwise now and then)
             ph[e] = (_Float16)pf;
             if (PL == 2) plo[e] = (_Float16)(pf - (float)ph[e]);
         }
         l = l * so + sum;
-        m = mn; mo = mon;
+        m = mn; d = dn;
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[t] *= turn;
         weigh(ph, plo, seen, 1.f);
@@ -517,18 +536,20 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
     // ---- the waves of a workgroup, in wave order ----
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (g == 0) { m_all[wave][c] = m; mo_all[wave][c] = mo; l_all[wave][c] = l; }
+    if (g == 0) { m_all[wave][c] = m; d_all[wave][c] = d; l_all[wave][c] = l; }
     __syncthreads();
     float *dst = part + ((size_t)head * gridDim.y + blockIdx.y) * kv8_record(HD);
-    float M = -INFINITY, MO = -INFINITY, den = 0.f;
+    float M = -INFINITY, D = -INFINITY, den = 0.f;
 #pragma unroll
-    for (int w = 0; w < KV8_WAVES; ++w) { M = fmaxf(M, m_all[w][c]); MO = fmaxf(MO, mo_all[w][c]); }
+    for (int w = 0; w < KV8_WAVES; ++w) M = fmaxf(M, m_all[w][c]);
 #pragma unroll
     for (int w = 0; w < KV8_WAVES; ++w) {
-        const float mw = m_all[w][c], lw = l_all[w][c];
-        den += mw == -INFINITY ? lw : kv8_exp2(mw - M) * lw;         // (lw is zero there, or NaN)
+        const float mw = m_all[w][c], lw = l_all[w][c], down = kv8_down(mw, M);
+        den += mw == -INFINITY ? lw : kv8_exp2(down) * lw;         // (lw is zero there, or NaN)
+        D = fmaxf(D, d_all[w][c] + down);
     }
-    const float mine = mo == -INFINITY ? 1.f : kv8_exp2(mo - MO), norm = kv8_exp2(MO - KV8_LIFT - M) / den;
+    D = M == -INFINITY ? 0.f : rintf(D);
+    const float mine = M == -INFINITY ? 1.f : kv8_exp2(kv8_down(m, M) + (d - D)), norm = kv8_exp2(D) / den;
     const int r = r0 + c, i = kv8_query(pl, r);
 #pragma unroll
     for (int t0 = 0; t0 < DT; t0 += CH) {
@@ -546,7 +567,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
             else kv8_out(out + ((size_t)b * pl.L + i) * ldo + ((size_t)head * pl.group + (r - i * pl.group)) * HD + d, a * norm, vec & 2);
         }
     }
-    if (pt.splits > 1 && wave == 0 && g == 0 && r < rows) { dst[RG * HD + c] = M; dst[RG * HD + RG + c] = MO; dst[RG * HD + 2 * RG + c] = den; }
+    if (pt.splits > 1 && wave == 0 && g == 0 && r < rows) { dst[RG * HD + c] = M; dst[RG * HD + RG + c] = D; dst[RG * HD + 2 * RG + c] = den; }
 }
 
 // Joins the splits of a pair.  64 units (four values of a row) a workgroup, KV8_JOIN threads each: a thread takes every KV8_JOIN-th split,
@@ -567,33 +588,31 @@ __global__ __launch_bounds__(64 * KV8_JOIN) void kv8_merge_kernel(const float *_
     const int u = (int)blockIdx.z * 64 + x, lr = u / (hd / 4), d = u % (hd / 4) * 4, r = r0 + lr;
     const bool live = lr < KV8_ROWS && r < rows;
     const float *e = src + KV8_ROWS * hd + lr;
-    float M = -INFINITY, MO = -INFINITY, den = 0.f;
+    float M = -INFINITY, D = 0.f, den = 0.f;
     f32x4 a = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](float ms, float ds, float ls, const f32x4 &v) {
+        const float Mn = fmaxf(M, ms);
+        const bool none = Mn == -INFINITY;
+        const float down = none ? 0.f : kv8_down(M, Mn), downs = none ? 0.f : kv8_down(ms, Mn), Dn = none ? D : rintf(fmaxf(D + down, ds + downs));
+        den = den * kv8_exp2(down) + ls * kv8_exp2(downs);             // (sums of nothing are zero, or NaN)
+        a = a * kv8_exp2(down + (D - Dn)) + v * kv8_exp2(downs + (ds - Dn));
+        M = Mn; D = Dn;
+    };
     if (live) {
 #pragma unroll 4
         for (int s = y; s < pt.splits; s += KV8_JOIN) {
-            const float ms = e[s * rec], mos = e[s * rec + KV8_ROWS], ls = e[s * rec + 2 * KV8_ROWS];
             const float4 v = *reinterpret_cast<const float4 *>(src + s * rec + lr * hd + d);
-            const float Mn = fmaxf(M, ms), MOn = fmaxf(MO, mos);
-            den = (M == -INFINITY ? den : den * kv8_exp2(M - Mn)) + (ms == -INFINITY ? ls : ls * kv8_exp2(ms - Mn));
-            a = a * (MO == -INFINITY ? 1.f : kv8_exp2(MO - MOn)) + (f32x4){v.x, v.y, v.z, v.w} * (mos == -INFINITY ? 1.f : kv8_exp2(mos - MOn));
-            M = Mn; MO = MOn;
+            add(e[s * rec], e[s * rec + KV8_ROWS], e[s * rec + 2 * KV8_ROWS], (f32x4){v.x, v.y, v.z, v.w});
         }
     }
-    red[y][0][x] = M; red[y][1][x] = MO; red[y][2][x] = den;
+    red[y][0][x] = M; red[y][1][x] = D; red[y][2][x] = den;
     acc[y][x] = a;
     __syncthreads();
     if (y || !live) return;
 #pragma unroll
-    for (int i = 1; i < KV8_JOIN; ++i) {
-        const float ms = red[i][0][x], mos = red[i][1][x], ls = red[i][2][x];
-        const float Mn = fmaxf(M, ms), MOn = fmaxf(MO, mos);
-        den = (M == -INFINITY ? den : den * kv8_exp2(M - Mn)) + (ms == -INFINITY ? ls : ls * kv8_exp2(ms - Mn));
-        a = a * (MO == -INFINITY ? 1.f : kv8_exp2(MO - MOn)) + acc[i][x] * (mos == -INFINITY ? 1.f : kv8_exp2(mos - MOn));
-        M = Mn; MO = MOn;
-    }
+    for (int i = 1; i < KV8_JOIN; ++i) add(red[i][0][x], red[i][1][x], red[i][2][x], acc[i][x]);
     const int i = kv8_query(pl, r);
-    kv8_out(out + ((size_t)b * pl.L + i) * ldo + ((size_t)head * pl.group + (r - i * pl.group)) * hd + d, a * (kv8_exp2(MO - KV8_LIFT - M) / den), vec & 2);
+    kv8_out(out + ((size_t)b * pl.L + i) * ldo + ((size_t)head * pl.group + (r - i * pl.group)) * hd + d, a * (kv8_exp2(D) / den), vec & 2);
 }
 
 static int kv8_plan(int n_seqs, int L, int n_heads, int n_kv, int hd, int cap, Kv8Plan *pl, int *slots_total)

@@ -498,3 +498,38 @@ def test_a_decoder_layer_of_these_operators(B):
 
 def up128(n):
     return -(-n // 128) * 128
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("scales", ["near", "apart"])
+@pytest.mark.parametrize("e", [18, 22, 24, 25, 26, 30, 60, 110])
+def test_scores_beyond_any_fraction(B, e, scales, dtype):
+    """Queries of 2^e and -2^e in one place, keys of four bits there: scores are exact, those that are largest are equal, all others are
+    lower by 2^e / (8 sqrt(hd)) and more and have no weight.  What is left is the mean of the values at the largest, off by the sums,
+    the common factor and one division: 2^-20 of the largest value.  bf16: the equal weights w = 2^x, where x is 12 only up to the rounding of a
+    reference of 2^e, are summed as they are and multiplied as one fp16, so the mean is off by fp16(w) / w, up to 2^-11; and it is rounded once more."""
+    hd, n, L = 64, 1500, 4
+    r = np.random.RandomState(e)
+
+    def change(kv):
+        p = kv.shape[1]
+        kv[:, :, 0] = 0
+        kv[0, :, 0, :, 0] = torch.from_numpy(1 + np.minimum(r.randint(0, 5, (p, 2)) + np.arange(p)[:, None] // 400, 7) / 8)      # rising
+        kv[:, :, 1] = rnd(e, *kv[:, :, 1].shape)
+        if scales == "apart":
+            for blk in range(p // 32 + 1):
+                kv[:, 32 * blk:32 * blk + 32, 1] *= 2.0 ** (9 * (blk % 5))
+
+    def only_one_place(q):
+        s = torch.tensor([1.0, -1.0, -1.0, 1.0])[:, None]
+        q.zero_()
+        q[:, ::hd] = s * 2.0 ** e
+
+    for cap, m, window in ((1600, n, 0), (1600, n, 700), (256, 150, 0), (4096, n, 0)):
+        c = Pair(B, 1, 2, hd, cap)
+        c.append([0], m + L, seed=80, change=change)
+        got, want, _, top = c.attend([m], L, 4, window=window, dtype=dtype, change=only_one_place)
+        room = (2.0 ** -20 + (2.0 ** -11 if dtype == "bf16" else 0)) * top
+        room = room + (2.0 ** -8 * (np.abs(want) + room) if dtype == "bf16" else 0)
+        assert np.isfinite(got).all(), (cap, m, window)
+        assert (np.abs(got - want) <= room).all(), (cap, m, window, np.max(np.abs(got - want) / room))
