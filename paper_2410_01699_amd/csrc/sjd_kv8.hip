@@ -271,6 +271,13 @@ __device__ __forceinline__ float kv8_log(float s, float cs, float shift)
     return fabsf(shift) >= KV8_FAR ? p + shift : fmaf(s, cs, shift);
 }
 
+// 2^d as two factors: the exponential has no subnormal results, the product with the second one has
+__device__ __forceinline__ void kv8_scale(float d, float &big, float &small)
+{
+    const float b = fmaxf(d, -100.f);
+    big = kv8_exp2(b); small = kv8_exp2(d - b);
+}
+
 // record of a split: O[KV8_ROWS][HD], then m, d and l of the rows; rows behind the last are not written
 __host__ __device__ __forceinline__ size_t kv8_record(int hd) { return (size_t)KV8_ROWS * (hd + 3); }
 
@@ -549,7 +556,10 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
         D = fmaxf(D, d_all[w][c] + down);
     }
     D = M == -INFINITY ? 0.f : rintf(D);
-    const float mine = M == -INFINITY ? 1.f : kv8_exp2(kv8_down(m, M) + (d - D)), norm = kv8_exp2(D) / den;
+    const float mine = M == -INFINITY ? 1.f : kv8_exp2(kv8_down(m, M) + (d - D));
+    float norm, tiny;
+    kv8_scale(D, norm, tiny);
+    norm /= den;
     const int r = r0 + c, i = kv8_query(pl, r);
 #pragma unroll
     for (int t0 = 0; t0 < DT; t0 += CH) {
@@ -564,7 +574,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
             const int d = (t0 + t) * 16 + g * 4;
             if (r >= rows) continue;
             if (pt.splits > 1) *reinterpret_cast<float4 *>(dst + c * HD + d) = make_float4(a[0], a[1], a[2], a[3]);
-            else kv8_out(out + ((size_t)b * pl.L + i) * ldo + ((size_t)head * pl.group + (r - i * pl.group)) * HD + d, a * norm, vec & 2);
+            else kv8_out(out + ((size_t)b * pl.L + i) * ldo + ((size_t)head * pl.group + (r - i * pl.group)) * HD + d, a * norm * tiny, vec & 2);
         }
     }
     if (pt.splits > 1 && wave == 0 && g == 0 && r < rows) { dst[RG * HD + c] = M; dst[RG * HD + RG + c] = D; dst[RG * HD + 2 * RG + c] = den; }
@@ -612,7 +622,9 @@ __global__ __launch_bounds__(64 * KV8_JOIN) void kv8_merge_kernel(const float *_
 #pragma unroll
     for (int i = 1; i < KV8_JOIN; ++i) add(red[i][0][x], red[i][1][x], red[i][2][x], acc[i][x]);
     const int i = kv8_query(pl, r);
-    kv8_out(out + ((size_t)b * pl.L + i) * ldo + ((size_t)head * pl.group + (r - i * pl.group)) * hd + d, a * (kv8_exp2(D) / den), vec & 2);
+    float norm, tiny;
+    kv8_scale(D, norm, tiny);
+    kv8_out(out + ((size_t)b * pl.L + i) * ldo + ((size_t)head * pl.group + (r - i * pl.group)) * hd + d, a * (norm / den) * tiny, vec & 2);
 }
 
 static int kv8_plan(int n_seqs, int L, int n_heads, int n_kv, int hd, int cap, Kv8Plan *pl, int *slots_total)

@@ -533,3 +533,22 @@ def test_scores_beyond_any_fraction(B, e, scales, dtype):
         room = room + (2.0 ** -8 * (np.abs(want) + room) if dtype == "bf16" else 0)
         assert np.isfinite(got).all(), (cap, m, window)
         assert (np.abs(got - want) <= room).all(), (cap, m, window, np.max(np.abs(got - want) / room))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("hd", [64, 256])
+@pytest.mark.parametrize("e", [-100, -110, -116, -122, -128, -134])
+def test_values_near_the_smallest(B, e, hd, dtype):
+    """outputs down to the types' subnormals, whole walks and joined ones; below 2^-126 an fp32 result is rounded to 2^-150, a bf16 one to 2^-134"""
+    def change(kv):
+        kv[:, :, 1] = rnd(81, *kv[:, :, 1].shape) * 2.0 ** e
+
+    for cap, n, L, window in ((256, 100, 3, 0), (2048, 1400, 2, 0), (2048, 1300, 2, 500)):
+        c = Pair(B, 1, 1, hd, cap)
+        c.append([0], n + L, seed=81, change=change)
+        got, want, mag, top = c.attend([n], L, 2, window=window, dtype=dtype)
+        d = (2.0 ** -22 + (hd + 8) * 2.0 ** -24) * mag
+        room = (np.expm1(2 * d) + 2.0 ** -20 + (2.0 ** -11 if dtype == "bf16" else 0)) * top + 2.0 ** -149
+        room = room + (2.0 ** -8 * (np.abs(want) + room) + 2.0 ** -134 if dtype == "bf16" else 0)
+        assert (np.abs(got - want) <= room).all(), (cap, np.max(np.abs(got - want) / room))
+        assert np.abs(want).max() > 2.0 ** (e - 6)
