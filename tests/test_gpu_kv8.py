@@ -552,3 +552,26 @@ def test_values_near_the_smallest(B, e, hd, dtype):
         room = room + (2.0 ** -8 * (np.abs(want) + room) + 2.0 ** -134 if dtype == "bf16" else 0)
         assert (np.abs(got - want) <= room).all(), (cap, np.max(np.abs(got - want) / room))
         assert np.abs(want).max() > 2.0 ** (e - 6)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_the_largest_finite_values_stay_when_their_block_grows(B, sign, dtype):
+    """Values from 248 * 2^120 on are kept as 256 * 2^120 = 2^128, which no float32 holds: the next window in their block keeps the code.
+    And with such a value among rejected ones only."""
+    big = sign * float(torch.finfo(TYPES[dtype]).max)
+    for at, n, what in ((2, 8, 1.0), (2, 8, -big), (9, 8, 1.0), (2, 8, float("inf")), (3, 31, 2.0 ** -60)):
+        def first(kv):
+            kv[0, at], kv[0, at + 1] = big, 250 * 2.0 ** 120 * sign
+
+        def second(kv):
+            kv[0, 1] = what
+
+        c = Pair(B, 1, 2, 64, 64, dtype)
+        c.append([0], max(n, 12), seed=82, change=first)
+        c.same()
+        with np.errstate(over="ignore"):
+            c.append([n], 5, seed=83, change=second)
+            c.same()
+            c.append([n + 2], 5, seed=84)
+        c.same()
