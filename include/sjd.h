@@ -396,7 +396,11 @@ int sjd_mx_product_test(int32_t rows, int32_t cols, int32_t slices, int32_t form
  * sjd_kv8_append: k, v dev [n_seqs * L][n_kv_heads * head_dim] (rows of length ld) into the cache.  The scale of a block that holds
  * positions already is made anew from those and the new ones; their codes move to it (exact but for codes that become
  * subnormal).  Positions of a touched block behind the window are zero afterwards; other blocks are not touched.  A window may be
- * appended again at the same or a smaller len (after a rejection).  len itself is the caller's to advance.        */
+ * appended again at the same or a smaller len (after a rejection).  len itself is the caller's to advance.
+ * So the cache is not strictly causal inside a block: keys and values that are more than 2^13 times smaller than the largest of their
+ * block, of a later position or of a draft too, are rounded to that one's grid, by up to 2^-16 of it, for the queries of the same forward
+ * already, and stay rounded when that position is rejected.  Where a decoder compares probabilities of two forwards, they differ by what
+ * that gives; values within 2^13 of each other keep their codes, and a block of 32 positions is not touched by any other.       */
 int sjd_kv8_append(int32_t dtype, const void *k, const void *v, int64_t ld, const int32_t *len, int32_t n_seqs, int32_t L,
                    int32_t n_kv_heads, int32_t head_dim, int32_t cap, uint8_t *cache, uint8_t *scales, void *stream);
 

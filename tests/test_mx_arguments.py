@@ -134,3 +134,25 @@ HOOK = dict(rows=64, cols=64, slices=1, format=8, codes=P, scales=P, packed=P, M
                                     dict(slices=2, ws=None), dict(slices=2, ws_bytes=16), dict(slices=2, ws=ODD)])
 def test_the_parity_entry_refuses(change):
     assert call("sjd_mx_product_test", HOOK, **change) == BAD
+
+
+def test_what_later_positions_do_to_a_block():
+    """the bounds that the header states for earlier codes of a block: kept within 2^13 of the largest magnitude appended to it, rejected ones
+    too, else off by at most 2^-16 of that (the reference moves codes as the kernel does, byte for byte)"""
+    import numpy as np
+    r = np.random.RandomState(4)
+    lost = 0
+    for case in range(60):
+        c = R.Cache(1, 1, 32, 32)
+        new = lambda L, e: (r.randn(1, L, 1, 32) * 2.0 ** r.uniform(*e, (1, L, 1, 1))).astype(np.float32).astype(np.float64)
+        first = new(4, (-20, 0))
+        c.append(first, first, [0], 4)
+        before, largest = c.values(0, 0, 4)[0], np.abs(first).max()
+        for n, e in ((4, (-3, 12)), (4, (5, 20)), (4, (-9, -2)), (9, (-20, 25))):             # a window, rejected twice, then kept
+            x = new(5, e)
+            c.append(x, x, [n], 5)
+            largest = max(largest, np.abs(x).max())
+            off = np.abs(c.values(0, 0, 4)[0] - before)
+            assert (off <= 2.0 ** -16 * largest).all() and (off[np.abs(before) >= 2.0 ** -13 * largest] == 0).all()
+        lost += np.count_nonzero(off)
+    assert lost
