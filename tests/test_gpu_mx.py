@@ -403,3 +403,19 @@ def test_the_binding_refuses(B):
         with pytest.raises(B.SjdError) as err:
             f()
         assert err.value.code == B.SJD_EINVAL, i
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("bits", [8, 4])
+def test_swiglu_of_gates_far_below_zero(B, bits, dtype):
+    """e^x below what fp32 holds, times values that bring it back: bf16 and fp32 hold the product"""
+    rows, F = 4, 256
+    r = np.random.RandomState(15)
+    gate = -np.linspace(60, 170, rows * F).reshape(rows, F)
+    y = np.exp2(r.randint(-60, 40, (rows, F // 32)).repeat(32, 1)) * (1 + r.rand(rows, F))       # the product's magnitude, much the same in a block
+    up = np.sign(r.randn(rows, F)) * np.clip(y / np.abs(gate) * np.exp(-gate), 1e-30, 1e38)
+    h = torch.from_numpy(np.concatenate((gate, up), 1)).to(TYPES[dtype]).cuda()
+    codes, scales = buffers(rows, F, bits)
+    B.sjd_mx_quantize(bits, h[:, :F], codes, scales, up=h[:, F:])
+    h = h.double().cpu().numpy()
+    near(h[:, :F] / (1 + np.exp(-h[:, :F])) * h[:, F:], codes_of(codes, bits), scales.cpu().numpy(), bits)
