@@ -136,7 +136,9 @@ extern "C" int sjd_kv8_append(int32_t dtype, const void *k, const void *v, int64
 {
     if (!k || !v || !len || !cache || !scales || (dtype != 0 && dtype != 1)) return SJD_EINVAL;
     if (!kv8_sizes(n_seqs, L, n_kv_heads, head_dim, cap) || ld < (int64_t)n_kv_heads * head_dim || !mx_aligned(cache) || !mx_aligned(scales)) return SJD_EINVAL;
-    const dim3 grid((L + 31) / 32 + 1, n_kv_heads, n_seqs * 2);
+    const int64_t blocks = ((int64_t)L + 31) / 32 + 1;
+    if (!mx_fits(blocks, 2 * head_dim)) return SJD_EINVAL;
+    const dim3 grid((unsigned)blocks, n_kv_heads, n_seqs * 2);
     // (loads of 16 bytes: rows aligned, and a block's within 32-bit offsets)
     const int vec = mx_vec(k, ld, dtype) && mx_vec(v, ld, dtype) && ld <= MX_OOB / 256, nblk = (cap + 31) / 32;
     hipStream_t s = (hipStream_t)stream;

@@ -339,12 +339,13 @@ struct MxTile { int bm, bn; struct { double fixed, step; } one, several; };
 static const MxTile mx_tiles[] = {{64, 64, {3.4, 0.33}, {3.4, 0.226}}, {64, 128, {4.7, 0.364}, {4.5, 0.307}}, {64, 192, {5.9, 0.41}, {5.7, 0.38}},
                                   {128, 128, {7.1, 0.517}, {7.9, 0.51}}, {128, 192, {8.4, 0.77}, {9.5, 0.633}}, {128, 256, {7.8, 0.864}, {13.9, 0.933}},
                                   {256, 256, {12.3, 1.46}, {1.7, 1.82}}};
-struct MxPlan { int kind, tn, mt, slices, per, wgs; };      // kind: -1 few rows, else the tile
+#define MX_NO_KERNEL -2
+struct MxPlan { int kind, tn, mt, slices, per, wgs; };      // kind: -1 few rows, MX_NO_KERNEL: no grid holds the product, else the tile
 static MxPlan mx_plan(int M, int N, int K)
 {
     const int steps = mx_up(K, 128) / 128, groups = mx_groups(K);
-    const double tiles = (N + 15) / 16, stream = (double)N * K * 0.53 / 5.5e6;          // us from memory
-    MxPlan best = {-1, 1, 1, 1, 0, 0};
+    const double tiles = std::ceil(N / 16.0), stream = (double)N * K * 0.53 / 5.5e6;          // us from memory
+    MxPlan best = {MX_NO_KERNEL, 0, 0, 1, 0, 0};
     double cost = 1e30;
     auto take = [&](double t, const MxPlan &p) { if (t < cost) { cost = t; best = p; } };
     const int mt = M <= 16 ? 1 : 2;
@@ -378,13 +379,15 @@ static int mx_product_args(int32_t format, const uint8_t *codes, const uint8_t *
     if ((format != SJD_MX8 && format != SJD_MX4) || (dtype != 0 && dtype != 1)) return SJD_EINVAL;
     return mx_aligned(codes) && mx_aligned(scales) && mx_aligned(packed) ? SJD_OK : SJD_EINVAL;
 }
-static size_t mx_product_bytes(const MxPlan &p, int M, int N) { return p.slices > 1 ? (size_t)p.slices * M * mx_up(N, 4) * sizeof(float) : 0; }
+static int64_t mx_quads(int N) { return ((int64_t)N + 3) / 4; }
+static size_t mx_product_bytes(const MxPlan &p, int M, int N) { return p.slices > 1 ? (size_t)p.slices * M * mx_quads(N) * sizeof(float4) : 0; }
 
 extern "C" int sjd_mx_product_workspace(int32_t M, int32_t N, int32_t K, size_t *bytes)
 {
     if (!bytes || M < 1 || N < 1 || K < 1 || K > SJD_MX_MAX_K) return SJD_EINVAL;
-    *bytes = mx_product_bytes(mx_plan(M, N, K), M, N);
-    return SJD_OK;
+    const MxPlan p = mx_plan(M, N, K);
+    *bytes = mx_product_bytes(p, M, N);
+    return p.kind == MX_NO_KERNEL ? SJD_EINVAL : SJD_OK;
 }
 
 // The sums of C on the kernel that `p` names; arguments are checked
@@ -392,7 +395,9 @@ static int mx_product_on(const MxPlan &p, int32_t format, const uint8_t *codes, 
                          int32_t dtype, void *C, int64_t ldc, void *workspace, void *stream)
 {
     const int Kp = mx_up(K, 128), tiles = (int)(((int64_t)N + 15) / 16), groups = mx_groups(K);
-    if (!mx_fits(p.kind < 0 ? ((int64_t)tiles + p.tn - 1) / p.tn : p.wgs, 512)) return SJD_EINVAL;
+    if (p.kind == MX_NO_KERNEL || !mx_fits(p.kind < 0 ? ((int64_t)tiles + p.tn - 1) / p.tn : p.wgs, 512)) return SJD_EINVAL;
+    const int64_t joins = ((int64_t)M * mx_quads(N) + 255) / 256;
+    if (p.slices > 1 && !mx_fits(joins, 256)) return SJD_EINVAL;
     const int vec = (uintptr_t)C % (dtype ? 8 : 16) == 0 && ldc % 4 == 0;
     hipStream_t s = (hipStream_t)stream;
     float *part = (float *)workspace;
@@ -419,7 +424,7 @@ static int mx_product_on(const MxPlan &p, int32_t format, const uint8_t *codes, 
 #undef ROWS
     HIP_TRY(hipGetLastError());
     if (p.slices > 1) {
-        const dim3 grid((unsigned)(((int64_t)M * (mx_up(N, 4) / 4) + 255) / 256));
+        const dim3 grid((unsigned)joins);
         if (dtype == 0) SJD_LAUNCH((mx_join_kernel<float>), grid, dim3(256), 0, s, (const float *)part, p.slices, M, N, (float *)C, ldc, vec);
         else SJD_LAUNCH((mx_join_kernel<bf16_t>), grid, dim3(256), 0, s, (const float *)part, p.slices, M, N, (bf16_t *)C, ldc, vec);
         HIP_TRY(hipGetLastError());
@@ -441,6 +446,7 @@ extern "C" int sjd_mx_product_plan(int32_t M, int32_t N, int32_t K, int32_t *row
 {
     if (!rows || !cols || !slices || M < 1 || N < 1 || K < 1 || K > SJD_MX_MAX_K) return SJD_EINVAL;
     const MxPlan p = mx_plan(M, N, K);
+    if (p.kind == MX_NO_KERNEL) return SJD_EINVAL;
     *rows = p.kind < 0 ? 16 * p.mt : mx_tiles[p.kind].bm;
     *cols = p.kind < 0 ? 16 * p.tn : mx_tiles[p.kind].bn;
     *slices = p.slices;
@@ -452,7 +458,7 @@ extern "C" int sjd_mx_product_test(int32_t rows, int32_t cols, int32_t slices, i
                                    size_t workspace_bytes, void *stream)
 {
     SJD_TRY(mx_product_args(format, codes, scales, packed, M, N, K, dtype, C, ldc));
-    MxPlan p = {-2, 0, 0, 1, 0, 0};
+    MxPlan p = {MX_NO_KERNEL, 0, 0, 1, 0, 0};
     if (rows <= 32) {
         const int tn = cols / 16;
         if ((rows != 16 && rows != 32) || cols != 16 * tn || tn < 1 || tn > (rows == 16 ? 6 : 4) || tn == 5 || slices != 1 || M > 32 * 65535) return SJD_EINVAL;
@@ -466,7 +472,7 @@ extern "C" int sjd_mx_product_test(int32_t rows, int32_t cols, int32_t slices, i
         const int steps = mx_up(K, 128) / 128, per = mx_up((steps + slices - 1) / slices, 4);
         p = {k, 0, 0, (steps + per - 1) / per, per, (int)wgs};
     }
-    if (p.kind == -2) return SJD_EINVAL;
+    if (p.kind == MX_NO_KERNEL) return SJD_EINVAL;
     const size_t need = mx_product_bytes(p, M, N);
     if (need && (!workspace || workspace_bytes < need || !mx_aligned(workspace))) return SJD_EINVAL;
     return mx_product_on(p, format, codes, scales, packed, M, N, K, dtype, C, ldc, workspace, stream);

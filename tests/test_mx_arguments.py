@@ -156,3 +156,25 @@ def test_what_later_positions_do_to_a_block():
             assert (off <= 2.0 ** -16 * largest).all() and (off[np.abs(before) >= 2.0 ** -13 * largest] == 0).all()
         lost += np.count_nonzero(off)
     assert lost
+
+
+@pytest.mark.parametrize("name,args,change", [
+    ("sjd_kv8_append", APPEND, dict(L=1 << 28, cap=1 << 28, hd=256, ld=512)),                     # 2^23 + 1 workgroups of 512
+    ("sjd_kv8_append", APPEND, dict(L=2 ** 31 - 65, cap=2 ** 31 - 65, hd=64)),
+    ("sjd_mx_product", PRODUCT, dict(M=2 ** 31 - 1, N=1 << 17, ldc=1 << 17)),                      # no kernel has a grid for that
+    ("sjd_mx_product", PRODUCT, dict(M=2 ** 31 - 1, N=2 ** 31 - 1, ldc=1 << 31)),
+    ("sjd_mx_product_test", HOOK, dict(slices=2, M=1 << 20, N=1 << 14, ldc=1 << 14, ws_bytes=1 << 60)),          # 2^32 threads that join
+])
+def test_launches_that_no_grid_holds_are_refused(name, args, change):
+    assert call(name, args, **change) == BAD
+
+
+def test_workspaces_of_the_widest_products():
+    """sizes whose tiles or padded columns pass 32 bits: no size that has wrapped around, an error where no kernel has a grid"""
+    for M, N in ((1, 2 ** 31 - 1), (33, 2 ** 31 - 1), (100, 2 ** 31 - 2), (2 ** 31 - 1, 1)):
+        assert B.sjd_mx_product_workspace(M, N, 4096) <= 4 * M * 2 ** 31 * 4
+        assert B.sjd_mx_product_plan(M, N, 4096) in PLANS
+    for f in (B.sjd_mx_product_workspace, B.sjd_mx_product_plan):
+        with pytest.raises(B.SjdError) as e:
+            f(2 ** 31 - 1, 2 ** 31 - 1, 4096)
+        assert e.value.code == BAD
