@@ -417,7 +417,11 @@ def _coded(dev, format, rows, K, codes, scales):
 
 
 def _workspace(dev, workspace, need):
-    return (_flat(dev, "workspace", workspace, need, more=True), workspace.numel()) if need else (None, 0)
+    if not need:
+        return None, 0
+    if workspace is None:
+        _refuse(f"a workspace of {need} bytes is needed")
+    return _flat(dev, "workspace", workspace, need, more=True), workspace.numel()
 
 
 def _matrix(name, t):

@@ -131,3 +131,17 @@ def test_what_the_hook_refuses(B):
         with pytest.raises(B.SjdError) as e:
             run(B, plan, gpu, 40, 100, 512, 8, "fp32")
         assert e.value.code == B.SJD_EINVAL, plan
+
+
+def test_a_missing_workspace_is_refused(B):
+    n = torch.zeros(1, dtype=torch.int32, device="cuda")
+    x = torch.zeros(1, 64, device="cuda")
+    cache, scales = (torch.zeros(64 * m, dtype=torch.uint8, device="cuda") for m in (64 * 64, 2))
+    M, N, K = 128, 4096, 11008
+    assert B.sjd_mx_product_workspace(M, N, K) > 0
+    gpu = [torch.zeros(m, dtype=torch.uint8, device="cuda") for m in (M * K, M * K // 32, B.sjd_mx_weights_bytes(N, K))]
+    for f in (lambda: B.sjd_kv8_attention(x, cache, scales, n, 1, 1, 1, 64, 2048, 0, 0, torch.zeros_like(x), None),
+              lambda: B.sjd_mx_product(8, *gpu, K, torch.zeros(M, N, device="cuda"), None)):
+        with pytest.raises(B.SjdError) as e:
+            f()
+        assert e.value.code == B.SJD_EINVAL

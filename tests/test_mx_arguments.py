@@ -178,3 +178,10 @@ def test_workspaces_of_the_widest_products():
         with pytest.raises(B.SjdError) as e:
             f(2 ** 31 - 1, 2 ** 31 - 1, 4096)
         assert e.value.code == BAD
+
+
+def test_a_workspace_that_is_needed_and_missing_is_an_error_of_the_library():
+    with pytest.raises(B.SjdError) as e:
+        B._workspace(0, None, 64)
+    assert e.value.code == BAD
+    assert B._workspace(0, None, 0) == (None, 0)
