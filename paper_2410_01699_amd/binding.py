@@ -430,8 +430,13 @@ def _matrix(name, t):
     return t.shape
 
 
-def _on(stream):
-    return None if stream is None else stream.cuda_stream
+def _on(dev, stream):
+    """the stream's handle; a kernel on another device's stream would run there, on memory of this one"""
+    if stream is None:
+        return None
+    if stream.device_index != dev:
+        _refuse("the stream is another device's")
+    return stream.cuda_stream
 
 
 def _done(rc):
@@ -450,7 +455,7 @@ def sjd_mx_quantize(format, x, codes, scales, up=None, stream=None):
         if du != dt or lu != ld:
             _refuse("x and up have the same type and stride")
     pc, ps = _coded(dev, format, rows, K, codes, scales)
-    _done(_lib.sjd_mx_quantize(format, dt, px, pu, ld, rows, K, pc, ps, _on(stream)))
+    _done(_lib.sjd_mx_quantize(format, dt, px, pu, ld, rows, K, pc, ps, _on(dev, stream)))
 
 
 def sjd_mx_rmsnorm(format, x, resid, gain, eps, codes, scales, stream=None):
@@ -464,7 +469,7 @@ def sjd_mx_rmsnorm(format, x, resid, gain, eps, codes, scales, stream=None):
     if dr:
         _refuse("resid is float32")
     pc, ps = _coded(dev, format, rows, d, codes, scales)
-    _done(_lib.sjd_mx_rmsnorm(format, dt, px, ldx, pr, ldr, _flat(dev, "gain", gain, d, 0), eps, rows, d, pc, ps, _on(stream)))
+    _done(_lib.sjd_mx_rmsnorm(format, dt, px, ldx, pr, ldr, _flat(dev, "gain", gain, d, 0), eps, rows, d, pc, ps, _on(dev, stream)))
 
 
 @functools.lru_cache(maxsize=4096)
@@ -479,7 +484,7 @@ def sjd_mx_weights(W, packed, stream=None):
     dev = _device(W)
     N, K = _matrix("W", W)
     pw, dt, ld = _rows(dev, "W", W, N, K)
-    _done(_lib.sjd_mx_weights(dt, pw, ld, N, K, _flat(dev, "packed", packed, sjd_mx_weights_bytes(N, K)), _on(stream)))
+    _done(_lib.sjd_mx_weights(dt, pw, ld, N, K, _flat(dev, "packed", packed, sjd_mx_weights_bytes(N, K)), _on(dev, stream)))
 
 
 @functools.lru_cache(maxsize=4096)
@@ -497,7 +502,7 @@ def sjd_mx_product(format, codes, scales, packed, K, out, workspace, stream=None
     pc, ps = _coded(dev, format, M, K, codes, scales)
     pw = _flat(dev, "packed", packed, sjd_mx_weights_bytes(N, K))
     ws, ws_bytes = _workspace(dev, workspace, sjd_mx_product_workspace(M, N, K))
-    _done(_lib.sjd_mx_product(format, pc, ps, pw, M, N, K, dt, po, ld, ws, ws_bytes, _on(stream)))
+    _done(_lib.sjd_mx_product(format, pc, ps, pw, M, N, K, dt, po, ld, ws, ws_bytes, _on(dev, stream)))
 
 
 def sjd_mx_product_plan(M, N, K):
@@ -515,7 +520,7 @@ def sjd_mx_product_test(plan, format, codes, scales, packed, K, out, workspace, 
     pc, ps = _coded(dev, format, M, K, codes, scales)
     pw = _flat(dev, "packed", packed, sjd_mx_weights_bytes(N, K))
     ws, ws_bytes = _workspace(dev, workspace, plan[2] * M * ((N + 3) // 4 * 4) * 4 if plan[2] > 1 else 0)
-    _done(_lib.sjd_mx_product_test(*plan, format, pc, ps, pw, M, N, K, dt, po, ld, ws, ws_bytes, _on(stream)))
+    _done(_lib.sjd_mx_product_test(*plan, format, pc, ps, pw, M, N, K, dt, po, ld, ws, ws_bytes, _on(dev, stream)))
 
 
 def _kv8(dev, cache, scales, n_seqs, n_kv, hd, cap):
@@ -532,7 +537,7 @@ def sjd_kv8_append(k, v, length, L, n_kv, hd, cap, cache, scales, stream=None):
     if dt != dv or ld != lv:
         _refuse("k and v have the same type and stride")
     pc, ps = _kv8(dev, cache, scales, n_seqs, n_kv, hd, cap)
-    _done(_lib.sjd_kv8_append(dt, pk, pv, ld, _flat(dev, "length", length, n_seqs, "int32"), n_seqs, L, n_kv, hd, cap, pc, ps, _on(stream)))
+    _done(_lib.sjd_kv8_append(dt, pk, pv, ld, _flat(dev, "length", length, n_seqs, "int32"), n_seqs, L, n_kv, hd, cap, pc, ps, _on(dev, stream)))
 
 
 @functools.lru_cache(maxsize=4096)
@@ -553,4 +558,4 @@ def sjd_kv8_attention(q, cache, scales, length, L, n_heads, n_kv, hd, cap, windo
     pc, ps = _kv8(dev, cache, scales, n_seqs, n_kv, hd, cap)
     ws, ws_bytes = _workspace(dev, workspace, sjd_kv8_attention_workspace(n_seqs, L, n_heads, n_kv, hd, cap))
     _done(_lib.sjd_kv8_attention(dt, pq, ldq, pc, ps, _flat(dev, "length", length, n_seqs, "int32"), n_seqs, L, n_heads, n_kv, hd, cap, window, sinks,
-                                 po, ldo, ws, ws_bytes, _on(stream)))
+                                 po, ldo, ws, ws_bytes, _on(dev, stream)))

@@ -185,3 +185,13 @@ def test_a_workspace_that_is_needed_and_missing_is_an_error_of_the_library():
         B._workspace(0, None, 64)
     assert e.value.code == BAD
     assert B._workspace(0, None, 0) == (None, 0)
+
+
+def test_a_stream_of_another_device_is_refused():
+    class Stream:
+        cuda_stream, device_index = 5, 1
+
+    assert B._on(1, Stream) == 5 and B._on(1, None) is None
+    with pytest.raises(B.SjdError) as e:
+        B._on(0, Stream)
+    assert e.value.code == BAD
