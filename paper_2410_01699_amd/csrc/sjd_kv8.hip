@@ -167,6 +167,7 @@ extern "C" int sjd_kv8_append(int32_t dtype, const void *k, const void *v, int64
 #define KV8_LIFT 12.f    // a row's reference is its largest score less this: weights up to 2^KV8_TOP in fp16, 22 bits of hi + lo hold from
 #define KV8_TOP 15.f     // 2^-14 on, and 2^-37 of the largest below
 #define KV8_O_LIFT 14.f  // weights times value scales, where those differ: 22 bits hold from 2^-27 of the largest on
+#define KV8_NONE -3.4028234664e38f        // reference of a row that has seen nothing: finite, so that differences need no cases
 #define KV8_FAR 1048576.f        // references from here on: fp32 has 1/8 between scores
 
 // The queries of one sequence that read one cache head, L * (heads per cache head) rows with a query's heads next to each other, are cut
@@ -263,17 +264,13 @@ __device__ __forceinline__ float kv8_exp2(float x) { return __builtin_amdgcn_exp
 
 // reference for a largest score: far ones have no room for the lift (it would be rounded to more than fp16 holds)
 __device__ __forceinline__ float kv8_ref(float top) { return top - (fabsf(top) < KV8_FAR ? KV8_LIFT : 0.f); }
-// the exponent by which sums with reference m go down to reference M >= m; sums of nothing (m = -inf) go to zero, or stay NaN
-__device__ __forceinline__ float kv8_down(float m, float M) { return m == -INFINITY ? -INFINITY : m - M; }
-// what a score's product has added: less the reference, and nothing while no score is known
-__device__ __forceinline__ float kv8_shift(float m) { return m == -INFINITY ? 0.f : -m; }
-// log2 of a score's weight, s cs + shift.  Far references are roundings of a product, and s cs itself may be many powers of two beside it: the
+// log2 of a score's weight, s cs - m.  Far references are roundings of a product, and s cs itself may be many powers of two beside it: the
 // product is rounded likewise before it is compared.
-__device__ __forceinline__ float kv8_log(float s, float cs, float shift)
+__device__ __forceinline__ float kv8_log(float s, float cs, float m)
 {
     float p = s * cs;
     asm("" : "+v"(p));                             // (no fused multiply-add)
-    return fabsf(shift) >= KV8_FAR ? p + shift : fmaf(s, cs, shift);
+    return fabsf(m) >= KV8_FAR ? p - m : fmaf(s, cs, -m);
 }
 
 // 2^d as two factors: the exponential has no subnormal results, the product with the second one has
@@ -390,7 +387,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
     f32x4 o[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, d, l = 0.f;
+    float m = KV8_NONE, d, l = 0.f;
     const float qs = q_scale[c];
     const int pos = sp.n + kv8_query(pl, min(r0 + c, rows - 1));
     // S = K codes . Q, then the next block's keys are requested; whole: no row's mask hides anything of the block
@@ -454,8 +451,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
     // ---- value scales near the first one ----
     sb = __builtin_amdgcn_readfirstlane(sc);
     const int base = sb >> 8;
-    float shift = 0.f;
-    bool far = false;                            // any row of the wave has a far reference
+    bool far = true;                             // any row of the wave has a far reference, or none yet
     for (; v < v_end; v += KV8_WAVES) {
         sb = __builtin_amdgcn_readfirstlane(sc);
         const int up = (sb >> 8) - base;
@@ -480,21 +476,20 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
             }
         }
         if (__ballot(bm - m > KV8_TOP)) {
-            const float mn = fmaxf(m, kv8_ref(kv8_across(bm))), turn = mn == -INFINITY ? 1.f : kv8_exp2(kv8_down(m, mn));
+            const float mn = fmaxf(m, kv8_ref(kv8_across(bm))), turn = kv8_exp2(m - mn);
             l *= turn;
 #pragma unroll
             for (int t = 0; t < DT; ++t) o[t] *= turn;
             m = mn;
-            shift = kv8_shift(m);
-            far = __ballot(fabsf(shift) >= KV8_FAR) != 0;
+            far = __ballot(fabsf(m) >= KV8_FAR) != 0;
         }
         float x[8];
         if (whole && !far) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = kv8_exp2(fmaf(s[e >> 2][e & 3], cs, shift));
+            for (int e = 0; e < 8; ++e) x[e] = kv8_exp2(fmaf(s[e >> 2][e & 3], cs, -m));
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = seen >> e & 1 ? kv8_exp2(kv8_log(s[e >> 2][e & 3], cs, shift)) : 0.f;
+            for (int e = 0; e < 8; ++e) x[e] = seen >> e & 1 ? kv8_exp2(kv8_log(s[e >> 2][e & 3], cs, m)) : 0.f;
         }
         f16x8 ph, plo = {};
 #pragma unroll
@@ -521,17 +516,14 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
         }
         bm = kv8_across(bm);
         const float mn = fmaxf(m, kv8_ref(bm));
-        const bool none = mn == -INFINITY;                                   // nothing seen so far
-        const float down = none ? 0.f : kv8_down(m, mn);
-        const float dn = none ? d : rintf(fmaxf(d + down, kv8_down(bm, mn) + ev - KV8_O_LIFT));
+        const float down = m - mn, dn = rintf(fmaxf(d + down, bm - mn + ev - KV8_O_LIFT));
         const float so = kv8_exp2(down), turn = kv8_exp2(down + (d - dn));      // what the sums so far are rescaled by
-        const float f = none ? 0.f : kv8_exp2(fminf(ev - dn, 120.f));
-        shift = kv8_shift(mn);
+        const float f = kv8_exp2(fminf(ev - dn, 120.f));
         float sum = 0.f;
         f16x8 ph, plo = {};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float x = seen >> e & 1 ? kv8_exp2(kv8_log(s[e >> 2][e & 3], cs, shift)) : 0.f;
+            const float x = seen >> e & 1 ? kv8_exp2(kv8_log(s[e >> 2][e & 3], cs, mn)) : 0.f;
             sum += x;
             float pf = x * f;
             if (PL == 2) asm("" : "+v"(pf));     // (the product in fp32 for both parts: fused into the conversion to fp16 it rounds otherwise now and then)
@@ -551,17 +543,17 @@ __global__ __launch_bounds__(64 * KV8_WAVES, HD <= 128 ? 4 : 2) void kv8_attenti
     if (g == 0) { m_all[wave][c] = m; d_all[wave][c] = d; l_all[wave][c] = l; }
     __syncthreads();
     float *dst = part + ((size_t)head * gridDim.y + blockIdx.y) * kv8_record(HD);
-    float M = -INFINITY, D = -INFINITY, den = 0.f;
+    float M = KV8_NONE, D = -INFINITY, den = 0.f;
 #pragma unroll
     for (int w = 0; w < KV8_WAVES; ++w) M = fmaxf(M, m_all[w][c]);
 #pragma unroll
     for (int w = 0; w < KV8_WAVES; ++w) {
-        const float mw = m_all[w][c], lw = l_all[w][c], down = kv8_down(mw, M);
-        den += mw == -INFINITY ? lw : kv8_exp2(down) * lw;         // (lw is zero there, or NaN)
+        const float down = m_all[w][c] - M;
+        den += kv8_exp2(down) * l_all[w][c];                             // (sums of nothing are zero, or NaN)
         D = fmaxf(D, d_all[w][c] + down);
     }
-    D = M == -INFINITY ? 0.f : rintf(D);
-    const float mine = M == -INFINITY ? 1.f : kv8_exp2(kv8_down(m, M) + (d - D));
+    D = rintf(D);
+    const float mine = kv8_exp2(m - M + (d - D));
     float norm, tiny;
     kv8_scale(D, norm, tiny);
     norm /= den;
@@ -603,13 +595,11 @@ __global__ __launch_bounds__(64 * KV8_JOIN) void kv8_merge_kernel(const float *_
     const int u = (int)blockIdx.z * 64 + x, lr = u / (hd / 4), d = u % (hd / 4) * 4, r = r0 + lr;
     const bool live = lr < KV8_ROWS && r < rows;
     const float *e = src + KV8_ROWS * hd + lr;
-    float M = -INFINITY, D = 0.f, den = 0.f;
+    float M = KV8_NONE, D = 0.f, den = 0.f;
     f32x4 a = {0.f, 0.f, 0.f, 0.f};
     auto add = [&](float ms, float ds, float ls, const f32x4 &v) {
-        const float Mn = fmaxf(M, ms);
-        const bool none = Mn == -INFINITY;
-        const float down = none ? 0.f : kv8_down(M, Mn), downs = none ? 0.f : kv8_down(ms, Mn), Dn = none ? D : rintf(fmaxf(D + down, ds + downs));
-        den = den * kv8_exp2(down) + ls * kv8_exp2(downs);             // (sums of nothing are zero, or NaN)
+        const float Mn = fmaxf(M, ms), down = M - Mn, downs = ms - Mn, Dn = rintf(fmaxf(D + down, ds + downs));
+        den = den * kv8_exp2(down) + ls * kv8_exp2(downs);
         a = a * kv8_exp2(down + (D - Dn)) + v * kv8_exp2(downs + (ds - Dn));
         M = Mn; D = Dn;
     };
