@@ -72,20 +72,25 @@ __device__ __forceinline__ void kv8_append_block(const T *__restrict__ src, int6
     }
     if (held) {
         const float s = mx_pow2(was);
+        // Code 256 with the largest scale, what values from 248 * 2^120 on were rounded to, is 2^128: the largest float below gives the same
+        // scale and the same code again.
+        const bool over = __builtin_amdgcn_readfirstlane(was) >= 247;
         const uint32_t w[4] = {old.x, old.y, old.z, old.w};
+        float y[16];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], true);
-            float y[4] = {lo.x * s, lo.y * s, hi.x * s, hi.y * s};
+            y[4 * i] = lo.x * s; y[4 * i + 1] = lo.y * s; y[4 * i + 2] = hi.x * s; y[4 * i + 3] = hi.y * s;
+        }
+        if (over) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                int p, d;
-                // (code 256 with the largest scale, what values from 248 * 2^120 on were rounded to, is 2^128: the largest float below gives
-                // the same scale and the same code again)
-                if (isinf(y[j])) y[j] = copysignf(3.4028234664e38f, y[j]);
-                place(i >> 1, (i & 1) * 4 + j, p, d);
-                if (p < held) { tile[p * PITCH + d] = y[j]; amax = max(amax, mx_finite_bits(y[j])); }
-            }
+            for (int e = 0; e < 16; ++e) if (isinf(y[e])) y[e] = copysignf(3.4028234664e38f, y[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            int p, d;
+            place(e >> 3, e & 7, p, d);
+            if (p < held) { tile[p * PITCH + d] = y[e]; amax = max(amax, mx_finite_bits(y[e])); }
         }
     }
 #pragma unroll
