@@ -408,7 +408,8 @@ int sjd_kv8_append(int32_t dtype, const void *k, const void *v, int64_t ld, cons
  * included: softmax(q k / sqrt(head_dim)) v.  The query at position p sees the positions j <= p with, if window > 0, also
  * j > p - window or j < sinks.  Query head h reads cache head h / (n_heads / n_kv_heads).  out dev, like q, rows of length ldo,
  * of the same dtype (which also says how finely probabilities are held: 22 bits for fp32, 11 for bf16).  workspace:
- * sjd_kv8_attention_workspace bytes (may be 0).  n_seqs is at most 32767, n_seqs * ceil(L * n_heads / n_kv_heads / 16) at most 65535.  What masked positions hold, NaN included, does not reach `out`.               */
+ * sjd_kv8_attention_workspace bytes (may be 0).  n_seqs is at most 32767, n_seqs * ceil(L * n_heads / n_kv_heads / 16) at most 65535.
+ * Scores are fp32: one that overflows there gives NaN.  What masked positions hold, NaN included, does not reach `out`.               */
 int sjd_kv8_attention_workspace(int32_t n_seqs, int32_t L, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t cap,
                                 size_t *bytes);
 int sjd_kv8_attention(int32_t dtype, const void *q, int64_t ldq, const uint8_t *cache, const uint8_t *scales, const int32_t *len,

@@ -24,7 +24,7 @@ static bool kv8_sizes(int n_seqs, int L, int n_kv, int hd, int cap)
 // ---- append ---------------------------------------------------------------------------------
 // A workgroup makes the keys (or the values) of one block: new rows and the codes that the block holds already meet in LDS as fp32,
 // their largest magnitude gives the scale, and a thread then makes 16 bytes of the record.
-// Windows of 16 for 8 sequences, 32 heads of 128, fp32: 5.6 us, three waits for memory one after the other (the length, the rows and codes, the
+// Windows of 16 for 8 sequences, 32 heads of 128, fp32: 5.9 us, three waits for memory one after the other (the length, the rows and codes, the
 // stores' end) and the launch; 2000 bf16 rows of a prompt 11.4 us, 49 MB at 4.3 TB/s against a copy's 4.9.
 template <int HD, int WHICH, typename T>
 __device__ __forceinline__ void kv8_append_block(const T *__restrict__ src, int64_t ld, int held, int rows, int vec, uint8_t *__restrict__ rec,

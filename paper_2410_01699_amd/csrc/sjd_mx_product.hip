@@ -324,7 +324,8 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const float *__restrict__ 
 //  - few rows: 0.6 + (records / 8) (1.5 + 0.6 TN) for 16 rows, several workgroups on a CU a seventh less; for 32 rows 2 + 0.4 a workgroup +
 //    (records / 8) (2.6 + 0.95 TN).
 // Slices of K add their sums' way through memory and a launch.  What this takes is 0.7 % slower than the best of all over those shapes, 12 %
-// at most.  us, measured, the kernel chosen and the next best ones:
+// at most.  Results of fp32 issue every product of 8 bits twice and rows of 4 bits read half the LDS, which the plan does not know: it may miss
+// their best kernel by more (2048 x 22016 x 4096: 339 us fp32, 141 to 160 us from 4 bits).  us, measured, the kernel chosen and the next best ones:
 //   16 rows    22016 x 4096   rows 6 tiles 11.1   3 tiles 11.7, 1 tile 17.0           (weights alone 7.5)
 //   100        4096 x 4096    rows 4 tiles 8.4    64 x 64 in 2 slices 12.2, 64 x 64 14.2
 //   100        8192 x 1536    64 x 64 7.7         rows 4 tiles 9.0, 64 x 128 9.1
@@ -334,7 +335,7 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const float *__restrict__ 
 //   512        4096 x 4096    64 x 128 17.0       64 x 64 18.0, 128 x 128 23.6
 //   1024       8192 x 1536    128 x 256 19.2      128 x 128 20.4, 64 x 192 20.6
 //   2048       12288 x 4096   128 x 192 97.6      128 x 256 107, 128 x 128 112
-//   2048       22016 x 4096   256 x 256 177       128 x 192 180, 128 x 128 194
+//   2048       22016 x 4096   128 x 192 181       256 x 256 188, 128 x 128 190      (in turn, medians of 40; another day 180 and 177)
 struct MxTile { int bm, bn; struct { double fixed, step; } one, several; };
 static const MxTile mx_tiles[] = {{64, 64, {3.4, 0.33}, {3.4, 0.226}}, {64, 128, {4.7, 0.364}, {4.5, 0.307}}, {64, 192, {5.9, 0.41}, {5.7, 0.38}},
                                   {128, 128, {7.1, 0.517}, {7.9, 0.51}}, {128, 192, {8.4, 0.77}, {9.5, 0.633}}, {128, 256, {7.8, 0.864}, {13.9, 0.933}},

@@ -575,3 +575,34 @@ def test_the_largest_finite_values_stay_when_their_block_grows(B, sign, dtype):
             c.same()
             c.append([n + 2], 5, seed=84)
         c.same()
+
+
+def test_a_walk_is_cut_and_whole_from_replay_to_replay(B):
+    """one graph over a long cache: lengths from one to many splits, and sequences that sit out, between its replays"""
+    n_seqs, n_kv, heads, hd, cap, L = 2, 2, 4, 64, 4096, 3
+    c = Pair(B, n_seqs, n_kv, hd, cap)
+    c.append([0, 0], cap)
+    n = lengths([0, 0])
+    q = rnd(90, n_seqs * L, heads * hd).cuda()
+    out, eager = torch.empty_like(q), torch.empty_like(q)
+    ws = [torch.empty(B.sjd_kv8_attention_workspace(n_seqs, L, heads, n_kv, hd, cap), dtype=torch.uint8, device="cuda") for _ in range(2)]
+
+    def attend(out, ws, stream=None):
+        B.sjd_kv8_attention(q, c.codes, c.scales, n, L, heads, n_kv, hd, cap, 0, 0, out, ws, stream=stream)
+
+    mark = 7.1                                  # (no value of the cache: a query that sees one position gives its codes' values)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        attend(out, ws[0], torch.cuda.current_stream())
+    for m in ([0, 0], [4000, 10], [10, 1500], [-1, 3000], [4093, 4093], [4094, 700], [-1, -1], [1000, 1000]):
+        n.copy_(lengths(m))
+        out.fill_(mark); eager.fill_(mark); ws[0].fill_(0xFF); ws[1].fill_(0xFF)
+        attend(eager, ws[1])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager), m
+        for b, k in enumerate(m):
+            rows = out[b * L:(b + 1) * L]
+            left = rows == mark
+            assert left.all() if k < 0 or k + L > cap else torch.isfinite(rows).all() and not left.any(), m

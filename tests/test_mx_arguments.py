@@ -125,6 +125,14 @@ def test_plans_are_kernels_that_exist():
     assert B._lib.sjd_mx_product_plan(1, 1, 1, None, C.byref(n), C.byref(n)) == BAD
 
 
+@pytest.mark.parametrize("size,plan", [((16, 22016, 4096), (16, 96, 1)), ((100, 4096, 4096), (32, 64, 1)), ((100, 8192, 1536), (64, 64, 1)), ((100, 4096, 11008), (64, 128, 4)),
+                                       ((200, 4096, 4096), (64, 64, 1)), ((256, 12288, 4096), (64, 192, 1)), ((512, 4096, 4096), (64, 128, 1)),
+                                       ((1024, 8192, 1536), (128, 256, 1)), ((2048, 12288, 4096), (128, 192, 1)), ((2048, 22016, 4096), (128, 192, 1))])
+def test_plans_of_the_sizes_whose_times_the_source_gives(size, plan):
+    """the table beside the plan names the kernel that runs"""
+    assert B.sjd_mx_product_plan(*size) == plan
+
+
 HOOK = dict(rows=64, cols=64, slices=1, format=8, codes=P, scales=P, packed=P, M=40, N=16, K=640, dtype=0, C=P, ldc=16, ws=P, ws_bytes=1 << 30, stream=None)
 
 
