@@ -355,7 +355,8 @@ int sjd_mx_quantize(int32_t format, int32_t dtype, const void *x, const void *up
 
 /* h = resid + x, kept in resid (dev fp32 [rows x d], in and out); h / sqrt(mean(h^2) + eps) * gain -> codes,
  * scales in `format`.  gain dev fp32 [d].  x NULL: h = resid (dtype and ldx are ignored); resid NULL: h = x, and nothing is kept.
- * Not both.  Sums in fp32.                                                                          */
+ * Not both.  Sums of squares are fp32: a row of zeros with eps = 0 gives NaN, as the formula does, and so may rows whose squares underflow
+ * (below 1e-19) with eps = 0; rows whose squares overflow (above 1e19) give zeros.                   */
 int sjd_mx_rmsnorm(int32_t format, int32_t dtype, const void *x, int64_t ldx, float *resid, int64_t ldr, const float *gain,
                    float eps, int32_t rows, int32_t d, uint8_t *codes, uint8_t *scales, void *stream);
 
