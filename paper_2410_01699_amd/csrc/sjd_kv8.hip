@@ -278,10 +278,11 @@ __device__ __forceinline__ float kv8_log(float s, float cs, float m)
     return fabsf(m) >= KV8_FAR ? p - m : fmaf(s, cs, -m);
 }
 
-// 2^d as two factors: the exponential has no subnormal results, the product with the second one has
+// 2^d as two factors: the exponential has no subnormal results, the product with the second one has.  The first stays normal when it is
+// divided by a sum of weights (up to 2^15 for each of 2^31 positions).
 __device__ __forceinline__ void kv8_scale(float d, float &big, float &small)
 {
-    const float b = fmaxf(d, -100.f);
+    const float b = fmaxf(d, -60.f);
     big = kv8_exp2(b); small = kv8_exp2(d - b);
 }
 

@@ -606,3 +606,20 @@ def test_a_walk_is_cut_and_whole_from_replay_to_replay(B):
             rows = out[b * L:(b + 1) * L]
             left = rows == mark
             assert left.all() if k < 0 or k + L > cap else torch.isfinite(rows).all() and not left.any(), m
+
+
+@pytest.mark.parametrize("n_kv", [1, 4])
+@pytest.mark.parametrize("byte", [5, 27, 127, 240])
+def test_sums_of_millions_keep_their_bits(B, byte, n_kv):
+    """All weights are 2^12 and all values 1.5: sums of up to 2^24 / 1.5 of them are exact in fp32, partial ones added in trees keep 2^-23
+    each, and the mean is the value, also where 2^d over the sum of weights would be subnormal"""
+    hd, n = 32, 3000001
+    cap, at_v = n + 2, R.cache_at(hd)[1]
+    codes = torch.zeros(1, n_kv, -(-cap // 32), 64 * hd, dtype=torch.uint8, device="cuda")
+    codes[..., torch.from_numpy(at_v.reshape(-1)).cuda()] = 0x3C
+    scales = torch.full((1, n_kv, codes.shape[2], 2), byte, dtype=torch.uint8, device="cuda")
+    q, out = torch.ones(1, n_kv * hd, device="cuda"), torch.empty(1, n_kv * hd, device="cuda")
+    ws = torch.empty(B.sjd_kv8_attention_workspace(1, 1, n_kv, n_kv, hd, cap), dtype=torch.uint8, device="cuda")
+    B.sjd_kv8_attention(q, codes, scales, lengths([n]), 1, n_kv, n_kv, hd, cap, 0, 0, out, ws)
+    want = 1.5 * 2.0 ** (byte - 127)
+    assert np.abs(out.double().cpu().numpy() / want - 1).max() <= 2.0 ** -20
