@@ -417,6 +417,74 @@ int sjd_kv8_attention(int32_t dtype, const void *q, int64_t ldq, const uint8_t *
                       int32_t n_seqs, int32_t L, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t cap, int32_t window,
                       int32_t sinks, void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- operators around a layer's products, over a paged cache ---------------------------------------
+ * What a decoder layer does besides its products when its keys and values lie in pages: rotary positions, the append of new keys and
+ * values, the attention over them, and the norms, gate and residual scale between two blocks.  They stand beside the microscaled operators, for
+ * programs that build their own layers (sjd_step uses neither), keep everything in the type it comes in (dtype: 0 = fp32, 1 = bf16) and
+ * hold sums, statistics and angles in 32 bits or more.  They allocate nothing, do not synchronise and can be captured into a graph; workspaces hold
+ * nothing between calls, calls that may run at the same time need one each.  ld*: elements from one row to the next.  SJD_EINVAL: a size, type,
+ * alignment or workspace that does not fit, or a launch of 2^32 threads.
+ *
+ * Rotary positions.  A frequency is a whole number of 2^-64 turns a position, turns dev uint64 [rot_dim / 2]; a position's angle is their product
+ * modulo whole turns, exact however far the position is (any int32, negative ones too).  Pair i of a head, values (i, i + rot_dim / 2) or, interleaved = 1,
+ * (2 i, 2 i + 1), becomes magnitude * (a cos - b sin, b cos + a sin); values from rot_dim on stay.  rot_dim is even and at most head_dim.
+ * sjd_rope_turns fills a host table (no GPU needed), 2 <= rot_dim <= 256, 1 < theta <= 1e30, with f_i = theta^(-2 i / rot_dim) radians a position, scaled:
+ *   LINEAR  f_i / factor
+ *   BASE    theta * factor^(rot_dim / (rot_dim - 2)) in theta's place (rot_dim > 2)
+ *   PARTS   with n_i = original f_i / 2 pi turns in the trained context and w = (n_i - slow) / (fast - slow) cut to 0 .. 1: w f_i + (1 - w) f_i / factor
+ * (1 <= factor <= 1e6; a magnitude of 0.1 ln(factor) + 1 goes with PARTS where scores are to keep their spread.)  Other frequencies may be written into the
+ * table by hand.
+ *
+ * sjd_rope: x dev [rows x n_heads * head_dim] -> out, alike, rows turned by pos dev int32 [rows] (inverse = 1: by minus the angle, which is also the gradient).
+ * out may be x.  Any even head_dim up to 256.  Rows of 16-byte units with rot_dim % 16 = 0 and head_dim % 16 = 0 take the faster kernel.   */
+#define SJD_ROPE_PLAIN 0
+#define SJD_ROPE_LINEAR 1
+#define SJD_ROPE_BASE 2
+#define SJD_ROPE_PARTS 3
+int sjd_rope_turns(double theta, int32_t rot_dim, int32_t scaling, double factor, double original, double slow, double fast, uint64_t *turns);
+int sjd_rope(int32_t dtype, const void *x, int64_t ldx, void *out, int64_t ldo, const int32_t *pos, int32_t rows, int32_t n_heads, int32_t head_dim,
+             const uint64_t *turns, int32_t rot_dim, int32_t interleaved, float magnitude, int32_t inverse, void *stream);
+
+/* A pool of pages for one layer: cache dev [n_pages][n_kv_heads][page / 32] records of 64 * head_dim values of dtype, 16-byte aligned.  page: a power of two
+ * of positions, 32 .. 65536; head_dim: 32, 64, 96, 128 or 256.  Position p of sequence b is in page table[b][p / page] (table dev int32 [n_seqs x width]), there in
+ * record p % page / 32 of each head.  A record holds the keys, then the values of 32 positions in units of 16 bytes, E = 8 (bf16) or 4 (fp32) values:
+ *   K[p][d] at E (32 (d / E) + p) + d % E                                      (a unit: E dimensions of a position)
+ *   V[p][d] at 32 head_dim + E ((1024 / E) (d / 32) + 32 u + d % 32) + e       (a unit: a dimension of E positions)
+ *     bf16: p = 16 t + 8 j + 4 h + i, u = 2 t + h, e = 4 j + i                 fp32: u = p / 4, e = p % 4
+ * A call is about `rows` rows of n_seqs sequences: start dev int32 [n_seqs + 1], ascending, rows start[b] .. start[b + 1] - 1 are the new tokens of sequence b, any
+ * number from zero on, and stand at positions len[b] .. (len dev int32 [n_seqs], positions before them).  Rows outside all sequences are not touched.  A sequence with
+ * len < 0, or whose tokens do not fit its table row, sits out: neither its pages nor its rows of the outputs are touched.  Where a table names a
+ * page outside the pool nothing is stored, and nothing is seen.  len is the caller's to advance; tokens may be appended again at the same or a smaller len.  */
+typedef struct { int32_t dtype, n_kv_heads, head_dim, page, n_pages; } sjd_pages;
+
+/* k, v dev [rows x n_kv_heads * head_dim] (rows of length ld) into the pages, keys turned by their positions (turns NULL and rot_dim 0: as they are).  Other positions of the
+ * records keep what they hold; a page that is written belongs to one sequence of the call.  q dev [rows x n_heads * head_dim], turned likewise, goes to q_out (which may
+ * be q); both NULL: keys and values only.                                                        */
+int sjd_page_append(const sjd_pages *pages, const void *q, int64_t ldq, int32_t n_heads, void *q_out, int64_t ldqo, const void *k, const void *v, int64_t ld,
+                    int32_t rows, const int32_t *start, const int32_t *len, int32_t n_seqs, const int32_t *table, int32_t width, const uint64_t *turns,
+                    int32_t rot_dim, int32_t interleaved, float magnitude, void *cache, void *stream);
+
+/* Attention of the new tokens' queries q dev [rows x n_heads * head_dim] (as they are: turned already) over the pages, the tokens' own keys included:
+ * softmax(scale q k) v -> out, like q, rows of length ldo.  The query at position p sees the positions j <= p with, if window > 0, also j > p - window or j < sinks; one
+ * that sees nothing gives zeros.  Query head h reads cache head h / (n_heads / n_kv_heads).
+ * Groups: the sequences groups[g] .. groups[g + 1] - 1 (groups dev int32 [n_groups + 1], ascending) begin with the same prefix[g] positions (dev int32 [n_groups]) in
+ * the same pages, say images of one prompt: what whole records of 32 positions of it hold is read and weighed once for all of them.  It may be claimed only where
+ * their table rows do name the same pages that far.  The result does not depend on it but for the order of sums.  n_groups 0: none.  With window > 0 groups are not used.
+ * scale is finite and above zero.  Scores and sums are fp32, bf16 probabilities have at least 8 bits; scores that overflow give NaN, as does a visible infinity or NaN among the
+ * values.  What masked positions hold, NaN included, does not reach `out`.  workspace: sjd_page_attention_workspace bytes (may be 0), 16-byte aligned.
+ * rows <= 2^24, n_seqs <= 65535, heads <= 4096.                                                  */
+int sjd_page_attention_workspace(const sjd_pages *pages, int32_t rows, int32_t n_seqs, int32_t n_groups, int32_t n_heads, int32_t width, size_t *bytes);
+int sjd_page_attention(const sjd_pages *pages, const void *q, int64_t ldq, int32_t n_heads, int32_t rows, const int32_t *start, const int32_t *len, int32_t n_seqs,
+                       const int32_t *table, int32_t width, const int32_t *groups, const int32_t *prefix, int32_t n_groups, const void *cache, float scale,
+                       int32_t window, int32_t sinks, void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Between two blocks of a decoder: h = resid + scale * gate * x / sqrt(mean(x^2) + eps) * post, kept in resid (dev fp32 [rows x d], in and out); h / sqrt(mean(h^2) + eps) * pre -> out.
+ * x, out dev [rows x d] of dtype; post, pre dev fp32 [d]; gate dev of dtype, rows of length ldg (0: one row for all).  post NULL: x as it is; gate NULL: ones; pre and out
+ * NULL: h only.  out may be x.  d <= SJD_NORM_MAX_D.  Sums of squares are fp32: rows whose squares overflow give zeros.                       */
+#define SJD_NORM_MAX_D 16384
+int sjd_block_norm(int32_t dtype, const void *x, int64_t ldx, const float *post, const void *gate, int64_t ldg, float scale, float *resid, int64_t ldr,
+                   const float *pre, float eps, int32_t rows, int32_t d, void *out, int64_t ldo, void *stream);
+
 const char *sjd_strerror(int code);
 
 #ifdef __cplusplus

@@ -22,6 +22,8 @@ SJD_MAX_ROWS = 128          # rows one forward computes (window x contexts x ima
 SJD_MAX_SAMP_VOCAB = 32768
 SJD_MX8, SJD_MX4 = 8, 4     # microscaled formats: E4M3, E2M1
 SJD_MX_MAX_K = 1 << 20
+SJD_ROPE_PLAIN, SJD_ROPE_LINEAR, SJD_ROPE_BASE, SJD_ROPE_PARTS = 0, 1, 2, 3
+SJD_NORM_MAX_D = 16384
 
 EXPORTS = ["sjd_init_model", "sjd_free_model", "sjd_kv_create", "sjd_kv_free", "sjd_kv_reset", "sjd_kv_len",
            "sjd_kv_set_len", "sjd_prefill", "sjd_first_window", "sjd_step", "sjd_generate", "sjd_forward_logits",
@@ -31,7 +33,8 @@ EXPORTS = ["sjd_init_model", "sjd_free_model", "sjd_kv_create", "sjd_kv_free", "
            "sjd_generate_batch", "sjd_profile_steps_batch", "sjd_verify_static", "sjd_gemm_plan",
            "sjd_mx_quantize", "sjd_mx_rmsnorm", "sjd_mx_weights_bytes", "sjd_mx_weights", "sjd_mx_product_workspace", "sjd_mx_product",
            "sjd_mx_product_plan", "sjd_mx_product_test",
-           "sjd_kv8_append", "sjd_kv8_attention_workspace", "sjd_kv8_attention"]
+           "sjd_kv8_append", "sjd_kv8_attention_workspace", "sjd_kv8_attention",
+           "sjd_rope_turns", "sjd_rope", "sjd_page_append", "sjd_page_attention_workspace", "sjd_page_attention", "sjd_block_norm"]
 
 PROF_KINDS = ("gemm", "attention", "elementwise", "verify")
 
@@ -58,6 +61,11 @@ class sjd_stats(C.Structure):
 class sjd_profile(C.Structure):
     _fields_ = [("ms", C.c_double * 4), ("bytes", C.c_double * 4), ("launches", C.c_int64 * 4), ("steps", C.c_int32),
                 ("ms_gemm_back_to_back", C.c_double)]
+
+
+class sjd_pages(C.Structure):
+    """the shape of one layer's pool of pages"""
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_kv_heads", "head_dim", "page", "n_pages")]
 
 
 class SjdError(RuntimeError):
@@ -124,6 +132,14 @@ _SIG = {
     "sjd_kv8_attention_workspace": (C.c_int, [_i32, _i32, _i32, _i32, _i32, _i32, _P(_sz)]),
     "sjd_kv8_attention": (C.c_int, [_i32, _vp, _i64, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _sz,
                                     _vp]),
+    "sjd_rope_turns": (C.c_int, [C.c_double, _i32, _i32, C.c_double, C.c_double, C.c_double, C.c_double, _vp]),
+    "sjd_rope": (C.c_int, [_i32, _vp, _i64, _vp, _i64, _vp, _i32, _i32, _i32, _vp, _i32, _i32, C.c_float, _i32, _vp]),
+    "sjd_page_append": (C.c_int, [_P(sjd_pages), _vp, _i64, _i32, _vp, _i64, _vp, _vp, _i64, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _i32, C.c_float,
+                                  _vp, _vp]),
+    "sjd_page_attention_workspace": (C.c_int, [_P(sjd_pages), _i32, _i32, _i32, _i32, _i32, _P(_sz)]),
+    "sjd_page_attention": (C.c_int, [_P(sjd_pages), _vp, _i64, _i32, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _i32, _vp, C.c_float, _i32, _i32, _vp,
+                                     _i64, _vp, _sz, _vp]),
+    "sjd_block_norm": (C.c_int, [_i32, _vp, _i64, _vp, _vp, _i64, C.c_float, _vp, _i64, _vp, C.c_float, _i32, _i32, _vp, _i64, _vp]),
     "sjd_gemm_bench": (C.c_int, [_i32, _i32, _i32, _i32, _i32, _i32, _i32, _P(C.c_float)]),
 }
 for _name, (_res, _args) in _SIG.items():
@@ -377,7 +393,7 @@ def _device(t):
     """the current device, on which t has to be"""
     import torch
     if not _KINDS:
-        _KINDS.update({torch.float32: 0, torch.bfloat16: 1, torch.uint8: "uint8", torch.int32: "int32"})
+        _KINDS.update({torch.float32: 0, torch.bfloat16: 1, torch.uint8: "uint8", torch.int32: "int32", torch.int64: "int64"})
     dev = t.get_device()
     if dev < 0 or dev != torch.cuda.current_device():
         _refuse(f"a tensor is on {t.device}, which is not the current GPU")
@@ -559,3 +575,139 @@ def sjd_kv8_attention(q, cache, scales, length, L, n_heads, n_kv, hd, cap, windo
     ws, ws_bytes = _workspace(dev, workspace, sjd_kv8_attention_workspace(n_seqs, L, n_heads, n_kv, hd, cap))
     _done(_lib.sjd_kv8_attention(dt, pq, ldq, pc, ps, _flat(dev, "length", length, n_seqs, "int32"), n_seqs, L, n_heads, n_kv, hd, cap, window, sinks,
                                  po, ldo, ws, ws_bytes, _on(dev, stream)))
+
+
+# ---- operators around a layer's products, over a paged cache ---------------------------------------
+def sjd_rope_turns(theta, rot_dim, scaling=SJD_ROPE_PLAIN, factor=1.0, original=0.0, slow=1.0, fast=32.0) -> np.ndarray:
+    """host int64 [rot_dim / 2]: the frequencies in 2^-64 turns a position, to be copied to the GPU; needs no GPU"""
+    t = np.empty(max(int(rot_dim), 2) // 2, np.int64)
+    _check(_lib.sjd_rope_turns(theta, rot_dim, scaling, factor, original, slow, fast, _host(t)))
+    return t
+
+
+def _turns(dev, turns, head_dim):
+    """(address, rot_dim) of a table of frequencies"""
+    if turns is None:
+        return None, 0
+    return _flat(dev, "turns", turns, turns.numel(), "int64"), 2 * turns.numel()
+
+
+def sjd_rope(x, out, pos, head_dim, turns, interleaved=False, magnitude=1.0, inverse=False, stream=None):
+    """x, out: device [rows, n_heads * head_dim] (out may be x); pos: device int32 [rows]; turns: device int64 [rot_dim / 2]"""
+    dev = _device(x)
+    rows, cols = _matrix("x", x)
+    px, dt, ldx = _rows(dev, "x", x, rows, cols)
+    po, do, ldo = _rows(dev, "out", out, rows, cols)
+    if do != dt or head_dim < 1 or cols % head_dim:
+        _refuse("x and out have one type and whole heads")
+    pt, rot = _turns(dev, turns, head_dim)
+    _done(_lib.sjd_rope(dt, px, ldx, po, ldo, _flat(dev, "pos", pos, rows, "int32"), rows, cols // head_dim, head_dim, pt, rot, int(interleaved), magnitude,
+                        int(inverse), _on(dev, stream)))
+
+
+def _paged(dev, pages, start, length, table, cache):
+    """(n_seqs, width, addresses of start, length, table, cache)"""
+    n_seqs = length.numel()
+    if table.dim() != 2 or table.shape[0] != n_seqs:
+        _refuse(f"table is {tuple(table.shape)}: a row for each of {n_seqs} sequences is needed")
+    code = _KINDS.get(cache.dtype)
+    if cache.get_device() != dev or code != pages.dtype or not cache.is_contiguous():
+        _refuse(f"cache is {cache.dtype} on {cache.device}: the pool's type, contiguous, on the current device is needed")
+    if cache.numel() != pages.n_pages * pages.n_kv_heads * pages.page * 2 * pages.head_dim:
+        _refuse(f"cache is {tuple(cache.shape)}, which is not {pages.n_pages} pages")
+    width = table.shape[1]
+    return (n_seqs, width, _flat(dev, "start", start, n_seqs + 1, "int32"), _flat(dev, "length", length, n_seqs, "int32"),
+            _flat(dev, "table", table, n_seqs * width, "int32"), cache.data_ptr())
+
+
+def sjd_page_append(pages, k, v, start, length, table, cache, turns=None, interleaved=False, magnitude=1.0, q=None, q_out=None, stream=None):
+    """k, v: device [rows, n_kv_heads * head_dim]; q, q_out (may be one): device [rows, n_heads * head_dim]; start: int32 [n_seqs + 1], length: int32 [n_seqs],
+    table: int32 [n_seqs, width], all on the device"""
+    dev = _device(k)
+    rows, cols = _matrix("k", k)
+    if cols != pages.n_kv_heads * pages.head_dim:
+        _refuse(f"k has {cols} columns, the pool {pages.n_kv_heads} heads of {pages.head_dim}")
+    n_seqs, width, ps, pl, pt, pc = _paged(dev, pages, start, length, table, cache)
+    pk, dt, ld = _rows(dev, "k", k, rows, cols)
+    pv, dv, lv = _rows(dev, "v", v, rows, cols)
+    if dt != pages.dtype or dv != dt:
+        _refuse("k, v and the pool have one type")
+    if rows == 1:
+        lv = ld
+    if lv != ld:
+        _refuse("k and v have the same stride")
+    pq = pqo = None
+    ldq = ldqo = heads = 0
+    if q is not None or q_out is not None:
+        if q is None or q_out is None:
+            _refuse("q and q_out come together")
+        qcols = _matrix("q", q)[1]
+        pq, dq, ldq = _rows(dev, "q", q, rows, qcols)
+        pqo, do, ldqo = _rows(dev, "q_out", q_out, rows, qcols)
+        if dq != dt or do != dt or qcols % pages.head_dim:
+            _refuse("q and q_out have the pool's type and whole heads")
+        heads = qcols // pages.head_dim
+    pr, rot = _turns(dev, turns, pages.head_dim)
+    _done(_lib.sjd_page_append(C.byref(pages), pq, ldq, heads, pqo, ldqo, pk, pv, ld, rows, ps, pl, n_seqs, pt, width, pr, rot, int(interleaved), magnitude, pc,
+                               _on(dev, stream)))
+
+
+@functools.lru_cache(maxsize=4096)
+def _page_workspace(shape, rows, n_seqs, n_groups, n_heads, width) -> int:
+    n = _sz(0)
+    _check(_lib.sjd_page_attention_workspace(C.byref(sjd_pages(*shape)), rows, n_seqs, n_groups, n_heads, width, C.byref(n)))
+    return n.value
+
+
+def sjd_page_attention_workspace(pages, rows, n_seqs, n_groups, n_heads, width) -> int:
+    return _page_workspace((pages.dtype, pages.n_kv_heads, pages.head_dim, pages.page, pages.n_pages), rows, n_seqs, n_groups, n_heads, width)
+
+
+def sjd_page_attention(pages, q, start, length, table, cache, out, workspace, scale, window=0, sinks=0, groups=None, prefix=None, stream=None):
+    """q, out: device [rows, n_heads * head_dim]; groups: int32 [n_groups + 1] and prefix: int32 [n_groups] on the device, or neither"""
+    dev = _device(q)
+    rows, cols = _matrix("q", q)
+    if cols % pages.head_dim:
+        _refuse("q has whole heads")
+    n_seqs, width, ps, pl, pt, pc = _paged(dev, pages, start, length, table, cache)
+    pq, dt, ldq = _rows(dev, "q", q, rows, cols)
+    po, do, ldo = _rows(dev, "out", out, rows, cols)
+    if dt != pages.dtype or do != dt:
+        _refuse("q, out and the pool have one type")
+    pg = pp = None
+    n_groups, heads = 0, cols // pages.head_dim
+    if groups is not None or prefix is not None:
+        if groups is None or prefix is None:
+            _refuse("groups and prefix come together")
+        n_groups = prefix.numel()
+        pg, pp = _flat(dev, "groups", groups, n_groups + 1, "int32"), _flat(dev, "prefix", prefix, n_groups, "int32")
+    ws, ws_bytes = _workspace(dev, workspace, sjd_page_attention_workspace(pages, rows, n_seqs, n_groups, heads, width))
+    _done(_lib.sjd_page_attention(C.byref(pages), pq, ldq, heads, rows, ps, pl, n_seqs, pt, width, pg, pp, n_groups, pc, scale, window, sinks, po, ldo, ws, ws_bytes,
+                                  _on(dev, stream)))
+
+
+def sjd_block_norm(x, resid, eps, out=None, post=None, gate=None, scale=1.0, pre=None, stream=None):
+    """resid fp32 [rows, d] += scale * gate * norm(x) * post, in place; out = norm(resid) * pre.  gate: [rows, d] or [1, d]"""
+    dev = _device(x)
+    rows, d = _matrix("x", x)
+    px, dt, ldx = _rows(dev, "x", x, rows, d)
+    pr, dr, ldr = _rows(dev, "resid", resid, rows, d)
+    if dr:
+        _refuse("resid is float32")
+    pg = po = None
+    ldg = ldo = 0
+    if gate is not None:
+        g_rows = _matrix("gate", gate)[0]
+        pg, dg, ldg = _rows(dev, "gate", gate, 1 if g_rows == 1 else rows, d)
+        if dg != dt:
+            _refuse("gate has the type of x")
+        if g_rows == 1:
+            ldg = 0
+    if (out is None) != (pre is None):
+        _refuse("out and pre come together")
+    if out is not None:
+        po, do, ldo = _rows(dev, "out", out, rows, d)
+        if do != dt:
+            _refuse("out has the type of x")
+    _done(_lib.sjd_block_norm(dt, px, ldx, None if post is None else _flat(dev, "post", post, d, 0), pg, ldg, scale, pr, ldr,
+                              None if pre is None else _flat(dev, "pre", pre, d, 0), eps, rows, d, po, ldo, _on(dev, stream)))

@@ -25,7 +25,8 @@ COMMON = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-
 # the sampling file needs every fp32 operation rounded separately (bit-exact contract)
 PER_FILE = {"sjd_sample.hip": ["-ffp-contract=off"]}
 SOURCES = ["sjd_api.hip", "sjd_gemm.hip", "sjd_gemm_bf16.hip", "sjd_gemm_wide.hip", "sjd_gemm_span.hip", "sjd_layers.hip", "sjd_attention.hip", "sjd_sample.hip",
-           "sjd_mx.hip", "sjd_mx_product.hip", "sjd_kv8.hip"]
+           "sjd_mx.hip", "sjd_mx_product.hip", "sjd_kv8.hip",
+           "sjd_page.hip", "sjd_page_attention.hip", "sjd_block_norm.hip"]
 
 
 def build(verbose: bool = True) -> str:

@@ -1,0 +1,466 @@
+"""Rotary positions, the paged cache and its attention, the norms between blocks (GPU only), against page_reference.
+
+Tolerances.  A sine or cosine is off by at most 2^-22 (its series 2^-29, eight roundings of values up to 1), a turned value by 2^-22 + 2^-23 of |a| + |b|.
+Attention: a score is a sum of hd rounded products, off by d = (hd + 8) 2^-24 scale sum |q k|; a weight by a factor of e^(2 d) and 2^-20; sums of n weights are
+added four (fp32) or more at a time, n / 4 + 64 roundings.  bf16: weights to 2^-8.  Norms: sums of at most 64 values a thread and ten partial sums, 2^-17 with the root.
+bf16 results: 2^-8 of their value for their own rounding, fp32 ones 2^-24.
+"""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import page_reference as R  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2410_01699_amd import binding
+    return binding
+
+
+def rnd(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed))
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def own(want, dtype):
+    return np.abs(want) * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24)
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def table_of(B, rot, **kw):
+    t = B.sjd_rope_turns(10000.0, rot, **kw)
+    return t, torch.from_numpy(t).cuda()
+
+
+def near_turned(got, x, pos, t, dtype, interleaved, magnitude=1.0, inverse=False):
+    want = R.rotate(x, pos, t, interleaved, magnitude, inverse)
+    size = np.abs(x).copy()                             # |a| + |b| of each value's pair
+    rot = 2 * len(t)
+    one, two = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+    both = size[..., one] + size[..., two]
+    size[..., one] = size[..., two] = both
+    room = size * magnitude * 3 * 2.0 ** -23
+    room[..., rot:] = 0
+    room[..., :rot] += own(want, dtype)[..., :rot] + (room[..., :rot] if dtype == "bf16" else 0)
+    assert (np.abs(got - want) <= room).all(), np.max(np.abs(got - want) - room)
+
+
+# ---- rotary positions ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rows,heads,hd,rot,pad", [(1, 1, 64, 64, 0), (3, 5, 128, 128, 32), (7, 3, 128, 64, 8), (5, 2, 96, 96, 0), (4, 3, 64, 20, 0), (2, 2, 128, 2, 0), (3, 1, 256, 256, 1),
+                                                   (6, 9, 80, 48, 3), (2, 17, 6, 4, 0), (600, 40, 128, 128, 16), (601, 33, 64, 32, 0)])
+def test_rows_are_turned(B, rows, heads, hd, rot, pad, interleaved, dtype):
+    t, turns = table_of(B, rot)
+    x = rnd(1, rows, heads * hd + pad).to(TYPES[dtype]).cuda()
+    pos = torch.randint(-50, 200000, (rows,), generator=torch.Generator().manual_seed(2), dtype=torch.int32)
+    pos[0] = 0
+    if rows > 3:
+        pos[1], pos[2] = 2 ** 31 - 1, -2 ** 31
+    out = torch.full_like(x, 7.0)
+    B.sjd_rope(x[:, :heads * hd], out[:, :heads * hd], pos.cuda(), hd, turns, interleaved=interleaved)
+    assert (out[:, heads * hd:] == 7).all()
+    sample = list(range(min(rows, 8))) + list(range(max(8, rows - 4), rows))
+    near_turned(host(out[sample, :heads * hd]).reshape(len(sample), heads, hd), host(x[sample, :heads * hd]).reshape(len(sample), heads, hd), pos[sample].tolist(), t, dtype, interleaved)
+    y = x.clone()
+    B.sjd_rope(y[:, :heads * hd], y[:, :heads * hd], pos.cuda(), hd, turns, interleaved=interleaved)           # in place, the same bits
+    assert torch.equal(y[:, :heads * hd], out[:, :heads * hd]) and torch.equal(y[:, heads * hd:], x[:, heads * hd:])
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_the_inverse_is_the_gradient(B, interleaved):
+    """<g, R x'> - <g, R x> = <R^T g, x' - x>, for the formula and for differences"""
+    t, turns = table_of(B, 64, scaling=B.SJD_ROPE_PARTS, factor=16.0, original=4096.0)
+    x, g = rnd(3, 5, 2 * 96).cuda(), rnd(4, 5, 2 * 96).cuda()
+    pos = ints([0, 1, 77, 4097, 1000003])
+    back = torch.empty_like(g)
+    B.sjd_rope(g, back, pos, 96, turns, interleaved=interleaved, magnitude=1.25, inverse=True)
+    near_turned(host(back).reshape(5, 2, 96), host(g).reshape(5, 2, 96), pos.tolist(), t, "fp32", interleaved, 1.25, True)
+    step = 2.0 ** -2
+    for i in (0, 40, 63, 64, 95, 130):
+        a, b, hi, lo = torch.empty_like(x), torch.empty_like(x), x.clone(), x.clone()
+        hi[:, i] += step
+        lo[:, i] -= step
+        for src, dst in ((hi, a), (lo, b)):
+            B.sjd_rope(src, dst, pos, 96, turns, interleaved=interleaved, magnitude=1.25)
+        slope = (host(g) * (host(a) - host(b))).sum(-1) / (2 * step)
+        # (rows are off by 2^-21 of sums up to 2 * 8, divided by the step)
+        assert np.abs(slope - host(back)[:, i]).max() <= 2.0 ** -21 * 16 * np.abs(host(g)).max() / step
+
+
+# ---- the cache ----------------------------------------------------------------------------------
+class Paged:
+    """a pool on the GPU and its reference; sequences have `width` pages each, in a random order"""
+
+    def __init__(self, B, n_seqs, kv, hd, page, width, dtype, spare=2, seed=0):
+        self.B, self.kv, self.hd, self.page, self.dtype, self.bf16 = B, kv, hd, page, dtype, dtype == "bf16"
+        self.n_pages = n_seqs * width + spare
+        self.pages = B.sjd_pages(int(self.bf16), kv, hd, page, self.n_pages)
+        self.table = np.random.RandomState(seed).permutation(self.n_pages)[:n_seqs * width].reshape(n_seqs, width).astype(np.int32)
+        self.cache = (rnd(seed + 9, self.n_pages, kv, page // 32, 64 * hd)).to(TYPES[dtype]).cuda()
+        self.ref = host(self.cache)
+
+    def dev(self):
+        return torch.from_numpy(np.ascontiguousarray(self.table)).cuda()
+
+    def append(self, length, tokens, seed=1, heads=0, t=None, interleaved=False, magnitude=1.0, pad=0, behind=0, change=None, inplace=False):
+        start = np.concatenate(([0], np.cumsum(tokens))).astype(int)
+        rows, kv, hd = start[-1] + behind, self.kv, self.hd
+        x = rnd(seed, rows, (heads + 2 * kv) * hd + pad)
+        if change:
+            change(x)
+        x = x.to(TYPES[self.dtype]).cuda()
+        before = x.clone()
+        q, k, v = x[:, :heads * hd], x[:, heads * hd:(heads + kv) * hd], x[:, (heads + kv) * hd:(heads + 2 * kv) * hd]
+        q_out = None if not heads else q if inplace else torch.full((rows, heads * hd + 8), 7.0, dtype=x.dtype, device="cuda")[:, :heads * hd]
+        self.B.sjd_page_append(self.pages, k, v, ints(start.tolist()), ints(length), self.dev(), self.cache, turns=None if t is None else torch.from_numpy(t).cuda(),
+                               interleaved=interleaved, magnitude=magnitude, q=q if heads else None, q_out=q_out)
+        pos, live = np.zeros(rows, int), np.zeros(rows, bool)
+        for b, n in enumerate(length):
+            pos[start[b]:start[b + 1]] = np.arange(n, n + tokens[b])
+            live[start[b]:start[b + 1]] = R.fits(n, tokens[b], self.table.shape[1], self.page)
+        before = host(before)
+        kk, vv = before[:, heads * hd:(heads + kv) * hd].reshape(rows, kv, hd), before[:, (heads + kv) * hd:(heads + 2 * kv) * hd].reshape(rows, kv, hd)
+        want = self.ref.copy()
+        R.store(want, kk if t is None else R.rotate(kk, pos, t, interleaved, magnitude), vv, start, length, self.table, self.page, self.bf16)
+        got = host(self.cache)
+        same = want == self.ref
+        assert np.array_equal(got[same], self.ref[same])                      # nothing else is touched
+        if t is None:
+            assert np.array_equal(got, want)
+        else:                                       # keys to the rotation's tolerance: |a| + |b| is at most the row's two largest
+            big = 2 * np.abs(before).max() * magnitude
+            assert (np.abs(got - want) <= 6 * 2.0 ** -23 * big + own(want, self.dtype)).all()
+        if heads:
+            out = host(q_out).reshape(rows, heads, hd)
+            src = before[:, :heads * hd].reshape(rows, heads, hd)
+            if live.any():
+                near_turned(out[live], src[live], pos[live].tolist(), t, self.dtype, interleaved, magnitude)
+            assert np.array_equal(out[~live], src[~live] if inplace else np.full_like(out[~live], 7.0))
+        self.ref = got
+
+    def attend(self, length, tokens, heads, window=0, sinks=0, groups=None, prefix=None, seed=5, pad=0, behind=0, scale=None, change=None, graph=False):
+        start = np.concatenate(([0], np.cumsum(tokens))).astype(int)
+        rows, hd, scale = start[-1] + behind, self.hd, scale or 1 / np.sqrt(self.hd)
+        q = rnd(seed, rows, heads * hd + pad)
+        if change:
+            change(q)
+        q = q.to(TYPES[self.dtype]).cuda()
+        out = torch.full_like(q, 7.0)
+        n_groups = 0 if prefix is None else len(prefix)
+        ws = torch.full((self.B.sjd_page_attention_workspace(self.pages, rows, len(length), n_groups, heads, self.table.shape[1]),), 0xFF, dtype=torch.uint8, device="cuda")
+        args = (self.pages, q[:, :heads * hd], ints(start.tolist()), ints(length), self.dev(), self.cache, out[:, :heads * hd], ws, float(scale))
+        more = dict(window=window, sinks=sinks, groups=None if prefix is None else ints(groups), prefix=None if prefix is None else ints(prefix))
+        self.B.sjd_page_attention(*args, **more)
+        assert (out[:, heads * hd:] == 7).all()
+        return host(out[:, :heads * hd]).reshape(rows, heads, hd), host(q[:, :heads * hd]).reshape(rows, heads, hd), start, float(np.float32(scale))
+
+    def check(self, length, tokens, heads, window=0, sinks=0, **kw):
+        got, q, start, scale = self.attend(length, tokens, heads, window, sinks, **kw)
+        want, mag, top = R.attention(self.ref, q, start, length, self.table, self.page, scale, self.bf16, window, sinks)
+        out = np.isnan(want).all(-1)
+        assert (got[out] == 7).all()
+        d = (self.hd + 8) * 2.0 ** -24 * mag[..., None]
+        n = max(x + y for x, y in zip(length, tokens))
+        room = (np.expm1(2 * d) + 2.0 ** -20 + (n / 4 + 64) * 2.0 ** -24 + (2.0 ** -8 if self.bf16 else 0)) * top[..., None]
+        room = room + own(np.abs(want) + room, self.dtype)
+        assert np.isfinite(got[~out]).all()
+        assert (np.abs(got - want)[~out] <= room[~out]).all(), np.max((np.abs(got - want) / room)[~out])
+        return got
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("kv,hd,page,heads,rot,interleaved,pad", [(3, 64, 32, 6, 64, False, 0), (1, 128, 64, 4, 128, True, 0), (2, 96, 32, 0, 48, False, 16), (2, 256, 32, 2, 256, False, 0),
+                                                                (4, 32, 128, 4, 10, True, 0), (2, 128, 32, 3, 64, False, 3), (8, 128, 32, 64, 128, False, 0)])
+def test_append(B, kv, hd, page, heads, rot, interleaved, pad, dtype):
+    width = 256 // page
+    c = Paged(B, 5, kv, hd, page, width, dtype)
+    t = B.sjd_rope_turns(10000.0, rot)
+    c.append([0, 0, 0, 0, 0], [1, 0, 33, 100, 7], seed=1, heads=heads, t=t, interleaved=interleaved, pad=pad, behind=3)
+    c.append([1, 31, 33, 100, 63], [1, 2, 31, 64, 66], seed=2, heads=heads, t=t, interleaved=interleaved, magnitude=1.2, pad=pad)
+    c.append([-1, 255, 256, 250, 0], [3, 1, 1, 7, 5], seed=3, heads=heads, t=t, interleaved=interleaved, pad=pad, behind=1)      # three sit out
+    c.append([1, 31, 33, 100, 63], [5, 5, 5, 5, 5], seed=4, pad=pad)                    # over what is there, not turned
+    if heads:
+        c.append([2, 40, 35, 90, 60], [2, 1, 0, 9, 40], seed=5, heads=heads, t=t, interleaved=interleaved, pad=pad, inplace=True)
+
+
+def test_append_leaves_pages_that_are_not_the_pools(B):
+    c = Paged(B, 3, 2, 64, 32, 4, "bf16")
+    c.table[0, 1], c.table[1, 0], c.table[2, 3] = -1, c.n_pages, 2 ** 31 - 1
+    c.append([20, 0, 60], [40, 40, 68], t=B.sjd_rope_turns(10000.0, 64), heads=2)
+    c.check([20, 0, 60], [40, 40, 68], 4)
+    c.check([32, 0, 60], [1, 30, 3], 4, window=1)             # windows that show nothing give zeros
+    got, *_ = c.attend([32, 0, 60], [1, 30, 3], 4, window=1)
+    assert (got[:31] == 0).all() and (got[31:] != 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("hd", [32, 64, 96, 128, 256])
+@pytest.mark.parametrize("length,tokens,heads,kv,page", [([0], [1], 1, 1, 32), ([33, 0, 5], [1, 40, 0], 4, 2, 32), ([63, 64, 65, 31], [1, 1, 1, 1], 3, 1, 64), ([100, 7], [17, 5], 14, 2, 128)])
+def test_attention(B, length, tokens, heads, kv, page, hd, dtype):
+    c = Paged(B, len(length), kv, hd, page, max(1, 256 // page), dtype)
+    c.check(length, tokens, heads, behind=2)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("length,tokens,heads,kv,window,sinks", [
+    ([1300], [1], 4, 4, 0, 0), ([1990], [3], 8, 1, 0, 0), ([1500, 3, 700, 1100], [1, 1, 2, 16], 4, 2, 0, 0), ([1500, 40, 1030], [5, 60, 1], 4, 2, 100, 0),
+    ([1500, 40, 1030], [5, 60, 1], 4, 2, 33, 40), ([1900, 5], [2, 9], 2, 2, 1, 0), ([1700, 1701], [1, 1], 2, 1, 1024, 4), ([1600], [70], 4, 4, 1, 1), ([64], [400], 2, 1, 0, 0),
+    ([0, 64, 0], [500, 200, 130], 6, 2, 0, 0), ([0, 300], [300, 150], 4, 1, 50, 7)])
+def test_attention_over_long_and_cut_walks(B, length, tokens, heads, kv, window, sinks, dtype):
+    c = Paged(B, len(length), kv, 64, 64, 32, dtype)
+    c.check(length, tokens, heads, window, sinks)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("hd,page", [(64, 32), (128, 64)])
+@pytest.mark.parametrize("width,length,tokens,groups,prefix", [
+    (32, [900, 950, 901], [1, 1, 2], [0, 3], [900]), (32, [900, 400, 410, 900], [1, 16, 3, 1], [1, 3], [400]), (32, [70, 70, 80, 900, 910], [3, 3, 3, 1, 2], [0, 3, 5], [70, 900]),
+    (8, [64, 100, 65], [1, 4, 1], [0, 3], [64]), (8, [100, 31], [1, 1], [0, 2], [31]), (8, [64, 33, 70], [9, 2, 9], [0, 2], [32]), (32, [500, 500], [1, 1], [0, 1], [500]),
+    (32, [500, -1, 640, 2000], [2, 2, 2, 60], [0, 4], [480]), (32, [-1, 500, 640], [2, 2, 2], [0, 3], [480]), (32, [0, 0], [200, 170], [0, 2], [128]), (32, [448, 448, 449], [30, 100, 1], [0, 3], [448])])
+def test_a_shared_prefix(B, width, length, tokens, groups, prefix, hd, page, dtype):
+    """as without groups; the first prefix[g] positions of a group lie in the same pages"""
+    width = width * 64 // page
+    c = Paged(B, len(length), 2, hd, page, width, dtype)
+    for g, p in enumerate(prefix):
+        c.table[groups[g]:groups[g + 1], :p // page] = c.table[groups[g], :p // page]
+        if p % page:                                            # (a page of which whole records are shared, the rest is each one's own: copied)
+            for b in range(groups[g] + 1, groups[g + 1]):
+                c.cache[c.table[b, p // page], :, :p % page // 32] = c.cache[c.table[groups[g], p // page], :, :p % page // 32]
+    c.ref = host(c.cache)
+    # tokens inside the prefix see it as well as those behind it
+    one = c.check(length, tokens, 8, groups=groups, prefix=prefix)
+    if any(R.fits(n, m, width, page) for n, m in zip(length, tokens)):
+        two = c.check(length, tokens, 8)
+        assert np.abs(np.nan_to_num(one) - np.nan_to_num(two)).max() < (0.1 if dtype == "bf16" else 1e-4)
+
+
+def test_groups_and_starts_of_no_sense_stay_inside(B):
+    """what device memory says is not trusted: whatever it holds, only rows of the call are written"""
+    c = Paged(B, 4, 2, 64, 32, 40, "bf16")
+    q, pad = rnd(3, 8, 256).to(torch.bfloat16).cuda(), torch.full((24, 256), 7.0, dtype=torch.bfloat16, device="cuda")
+    for start, groups, prefix, length in (([0, 8, 4, 6, 99], [0, 4], [1200], [1000, 20, 30, 5]), ([-5, 3, 2 ** 31 - 1, 0, 8], [2, 1, 9], [-7, 2 ** 31 - 1], [5, 5, 5, 5]),
+                                          ([0, 2, 4, 6, 8], [-3, 9], [2 ** 31 - 1], [2 ** 31 - 1, -2 ** 31, 1279, 1278]), ([0, 2, 4, 6, 8], [4, 4], [100], [100, 100, 100, 100])):
+        ws = torch.zeros(B.sjd_page_attention_workspace(c.pages, 8, 4, len(prefix), 4, 40), dtype=torch.uint8, device="cuda")
+        B.sjd_page_attention(c.pages, q, ints(start), ints(length), c.dev(), c.cache, pad[8:16], ws, 0.125, groups=ints(groups), prefix=ints(prefix))
+        k = rnd(4, 8, 128).to(torch.bfloat16).cuda()
+        B.sjd_page_append(c.pages, k, k, ints(start), ints(length), c.dev(), c.cache)
+    assert (pad[:8] == 7).all() and (pad[16:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_what_masks_hide_does_not_matter(B, dtype):
+    """NaN and infinities in masked positions, of the pages' unwritten rest and of later tokens"""
+    c = Paged(B, 2, 2, 64, 32, 40, dtype)
+    tokens, length = [3, 40], [50, 1100]
+    _, v = R.record_at(64, dtype == "bf16")
+    clean = c.check(length, tokens, 4)
+    for b, n in enumerate(length):
+        for p in range(n + tokens[b], (n + tokens[b] + 31) // 32 * 32):
+            rec = c.cache[c.table[b, p // 32], :, 0]
+            rec[:] = torch.where(torch.zeros_like(rec, dtype=torch.bool).index_fill_(1, torch.from_numpy(v[p % 32]).cuda(), True), float("nan") if p % 2 else float("inf"), rec)
+    got, *_ = c.attend(length, tokens, 4)
+    assert np.array_equal(got, clean)
+    # a NaN of the last token is seen by that one only
+    p = 1139
+    rec = c.cache[c.table[1, p // 32], :, 0]
+    rec[:, torch.from_numpy(v[p % 32][5:6]).cuda()] = float("nan")
+    got, *_ = c.attend(length, tokens, 4)
+    assert np.array_equal(got[:-1], clean[:-1])
+    assert np.isnan(got[-1][:, 5]).all() and np.array_equal(np.delete(got[-1], 5, 1), np.delete(clean[-1], 5, 1))
+
+
+def test_scores_far_from_zero(B):
+    """largest scores of 2^-20 to 2^24 and shifts of all of them: weights are differences"""
+    c = Paged(B, 2, 1, 64, 32, 40, "fp32")
+    for f in (-20, 0, 6, 12):
+        got, q, start, scale = c.attend([300, 1200], [1, 2], 2, scale=2.0 ** f)
+        assert np.isfinite(got).all()
+        want, mag, top = R.attention(c.ref, q, start, [300, 1200], c.table, 32, scale, False)
+        d = (64 + 8) * 2.0 ** -24 * mag[..., None]
+        assert (np.abs(got - want) <= (np.minimum(np.expm1(2 * d), 2.0) + 2.0 ** -14) * top[..., None]).all()
+
+
+def test_a_decoding_loop(B):
+    """prompts that share their first pages, windows of drafts, of which some are kept, single tokens: append, attend, norm, step by step"""
+    for dtype in ("fp32", "bf16"):
+        c = Paged(B, 3, 2, 64, 32, 20, dtype)
+        t = B.sjd_rope_turns(10000.0, 64)
+        c.table[1:, :3] = c.table[0, :3]
+        c.append([0, -1, -1], [100, 1, 1], heads=4, t=t, seed=50)                    # the prompt once; its fourth page is copied
+        for b in (1, 2):
+            c.cache[c.table[b, 3]] = c.cache[c.table[0, 3]]
+        c.ref = host(c.cache)
+        n = [100, 100, 100]
+        resid = rnd(60, 48, 256).cuda()
+        for i, (tokens, kept) in enumerate((([16, 16, 16], [3, 16, 1]), ([16, 5, 16], [7, 5, 2]), ([1, 1, 1], [1, 1, 1]), ([4, 0, 9], [4, 0, 9]))):
+            c.append(n, tokens, heads=4, t=t, seed=70 + i)
+            got = c.check(n, tokens, 4, groups=[0, 3], prefix=[100], seed=80 + i)
+            x = torch.from_numpy(got.reshape(len(got), -1)).to(TYPES[dtype]).cuda()
+            before, ones = host(resid[:len(x)]), torch.ones(256, device="cuda")
+            out = torch.empty_like(x)
+            B.sjd_block_norm(x, resid[:len(x)], 1e-5, out, post=ones, scale=0.5, pre=ones)
+            h, want, y = R.norm(host(x), before, 1e-5, np.ones(256), None, 0.5, np.ones(256))
+            assert (np.abs(host(out) - want) <= 2.0 ** -15 * (1 + np.abs(want)) + own(want, dtype)).all()
+            n = [a + k for a, k in zip(n, kept)]
+
+
+# ---- norms --------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,d,pad", [(1, 1, 0), (3, 64, 0), (2, 1536, 8), (5, 4096, 0), (3, 777, 0), (2, 2049, 3), (1, 8192, 0), (2, 16384, 0), (2, 16383, 0), (40, 100, 4)])
+@pytest.mark.parametrize("post,gate,pre", [(1, "rows", 1), (1, "vector", 1), (0, "none", 1), (0, "rows", 0), (1, "none", 0)])
+def test_block_norm(B, rows, d, pad, post, gate, pre, dtype):
+    t = TYPES[dtype]
+    x = (3 * rnd(1, rows, d + pad)).to(t).cuda()[:, :d]
+    resid = rnd(2, rows, d + pad).cuda()
+    resid[0, 0] = 300.0
+    keep = resid.clone()
+    p, r = 1 + 0.1 * rnd(3, d).cuda(), 1 + 0.1 * rnd(4, d).cuda()
+    g = {"none": None, "vector": rnd(5, 1, d).to(t).cuda(), "rows": rnd(6, rows, d + 2 * pad).to(t).cuda()[:, :d]}[gate]
+    out = torch.full((rows, d + pad), 7.0, dtype=t, device="cuda")
+    B.sjd_block_norm(x, resid[:, :d], 1e-5, out[:, :d] if pre else None, post=p if post else None, gate=g, scale=-0.75, pre=r if pre else None)
+    h, want, y = R.norm(host(x), host(keep[:, :d]), 1e-5, host(p) if post else None, None if g is None else host(g), -0.75, host(r) if pre else None)
+    room = np.abs(y) * 2.0 ** -17 + np.abs(h) * 2.0 ** -23
+    assert (np.abs(host(resid[:, :d]) - h) <= room).all()
+    assert torch.equal(resid[:, d:], keep[:, d:]) and (out[:, d:] == 7).all()
+    if pre:
+        rms = np.sqrt((h * h).mean(-1, keepdims=True) + 1e-5)
+        slack = np.abs(host(r)) / rms * room + np.abs(want) * (2.0 ** -17 + np.abs(room / np.maximum(rms, 1e-30)).max())
+        assert (np.abs(host(out[:, :d]) - want) <= slack + own(np.abs(want) + slack, dtype)).all()
+        z = x.clone()                                              # out may be x
+        again = keep.clone()
+        B.sjd_block_norm(z, again[:, :d], 1e-5, z, post=p if post else None, gate=g, scale=-0.75, pre=r)
+        assert torch.equal(z, out[:, :d]) and torch.equal(again, resid)
+
+
+# ---- as programs use them -------------------------------------------------------------------------
+def test_calls_are_captured_and_replayed(B):
+    """one graph of a layer's calls, replayed over other inputs, lengths and pages, with eager work between"""
+    c = Paged(B, 3, 2, 128, 32, 40, "bf16")
+    t = torch.from_numpy(B.sjd_rope_turns(10000.0, 128)).cuda()
+    rows, heads = 6, 8
+    q, k, v, out, turned = (torch.zeros(rows, n * 128, dtype=torch.bfloat16, device="cuda") for n in (heads, 2, 2, heads, heads))
+    start, length, table = ints([0, 1, 4, 6]), ints([5, 6, 7]), c.dev()
+    groups, prefix = ints([0, 3]), ints([64])
+    ws = torch.empty(B.sjd_page_attention_workspace(c.pages, rows, 3, 1, heads, 40), dtype=torch.uint8, device="cuda")
+    resid, gain = rnd(1, rows, heads * 128).cuda(), torch.ones(heads * 128, device="cuda")
+
+    def layer(cache, out, resid, stream):
+        B.sjd_page_append(c.pages, k, v, start, length, table, cache, turns=t, q=q, q_out=turned, stream=stream)
+        B.sjd_page_attention(c.pages, turned, start, length, table, cache, out, ws, 0.125, groups=groups, prefix=prefix, stream=stream)
+        B.sjd_block_norm(out, resid, 1e-5, out, post=gain, pre=gain, stream=stream)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        layer(c.cache, out, resid, s)
+    for i in range(4):
+        for x, seed in ((q, 10), (k, 20), (v, 30)):
+            x.copy_(rnd(seed + i, *x.shape))
+        length.copy_(ints([64 + 300 * i, 80, 1200 - i]))
+        tb = c.table.copy()
+        tb[:, :2] = tb[i % 3, :2]
+        table.copy_(torch.from_numpy(tb).cuda())
+        cache2, resid2, out2 = c.cache.clone(), resid.clone(), torch.empty_like(out)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        layer(cache2, out2, resid2, None)
+        torch.cuda.synchronize()
+        assert torch.equal(out, out2) and torch.equal(c.cache, cache2) and torch.equal(resid, resid2)
+
+
+def test_two_streams_at_once(B):
+    """calls on two streams with a workspace each give what they give alone"""
+    c = Paged(B, 4, 2, 128, 64, 40, "fp32")
+    q = rnd(1, 8, 4 * 128).cuda()
+    start, lens, table = ints([0, 2, 4, 6, 8]), [ints([2000, 1500, 100, 5]), ints([3, 2500, 2501, 700])], c.dev()
+    size = B.sjd_page_attention_workspace(c.pages, 8, 4, 0, 4, 40)
+    want = []
+    for n in lens:
+        o = torch.empty_like(q)
+        B.sjd_page_attention(c.pages, q, start, n, table, c.cache, o, torch.empty(size, dtype=torch.uint8, device="cuda"), 0.1)
+        want.append(o)
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream(), torch.cuda.Stream()], [torch.empty_like(q) for _ in range(2)]
+    ws = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            B.sjd_page_attention(c.pages, q, start, lens[i], table, c.cache, outs[i], ws[i], 0.1, stream=streams[i])
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
+def test_a_pool_beyond_32_bits(B):
+    """records behind 2^31 values and 2^32 bytes"""
+    kv, hd, page = 8, 128, 256
+    n_pages = 2 ** 31 // (kv * page * 2 * hd) + 40
+    pages = B.sjd_pages(1, kv, hd, page, n_pages)
+    cache = torch.zeros(n_pages, kv, page // 32, 64 * hd, dtype=torch.bfloat16, device="cuda")
+    table = ints([[n_pages - 1, 3, n_pages - 2]])
+    n, m = 500, 30
+    old = rnd(1, n, 2 * kv * hd).to(torch.bfloat16).cuda()
+    B.sjd_page_append(pages, old[:, :kv * hd], old[:, kv * hd:], ints([0, n]), ints([0]), table, cache)
+    new = rnd(2, m, 2 * kv * hd).to(torch.bfloat16).cuda()
+    B.sjd_page_append(pages, new[:, :kv * hd], new[:, kv * hd:], ints([0, m]), ints([n]), table, cache)
+    q, out = rnd(3, m, kv * hd).to(torch.bfloat16).cuda(), torch.empty(m, kv * hd, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(B.sjd_page_attention_workspace(pages, m, 1, 0, kv, 3), dtype=torch.uint8, device="cuda")
+    B.sjd_page_attention(pages, q, ints([0, m]), ints([n]), table, cache, out, ws, 0.09)
+    kvs = torch.cat((old, new)).double().view(n + m, 2, kv, hd)
+    s = torch.einsum("ihd,jhd->hij", q.double().view(m, kv, hd), kvs[:, 0]) * float(np.float32(0.09))
+    s = s.masked_fill(torch.arange(n + m, device="cuda") > torch.arange(n, n + m, device="cuda")[:, None], -torch.inf)
+    want = torch.einsum("hij,jhd->ihd", torch.softmax(s, -1), kvs[:, 1]).reshape(m, -1)
+    assert (out.double() - want).abs().max() <= 2.0 ** -7 * kvs.abs().max()
+
+
+def test_refusals_on_the_gpu(B):
+    c = Paged(B, 2, 2, 64, 32, 40, "bf16")
+    q, k, out = (torch.zeros(4, n, dtype=torch.bfloat16, device="cuda") for n in (256, 128, 256))
+    start, length, table = ints([0, 2, 4]), ints([3, 3]), c.dev()
+    ws = torch.empty(B.sjd_page_attention_workspace(c.pages, 4, 2, 1, 4, 40), dtype=torch.uint8, device="cuda")
+    t = torch.zeros(32, dtype=torch.int64, device="cuda")
+    bad = [
+        lambda: B.sjd_page_attention(c.pages, q.float(), start, length, table, c.cache, out, ws, 1.0),
+        lambda: B.sjd_page_attention(c.pages, q, start, length, table, c.cache.float(), out, ws, 1.0),
+        lambda: B.sjd_page_attention(c.pages, q, start, length, table, c.cache[1:], out, ws, 1.0),
+        lambda: B.sjd_page_attention(c.pages, q, start[:2], length, table, c.cache, out, ws, 1.0),
+        lambda: B.sjd_page_attention(c.pages, q, start, length, table[:1], c.cache, out, ws, 1.0),
+        lambda: B.sjd_page_attention(c.pages, q, start, length, table, c.cache, out, None, 1.0),
+        lambda: B.sjd_page_attention(c.pages, q, start, length, table, c.cache, out, ws[:64], 1.0),
+        lambda: B.sjd_page_attention(c.pages, q, start, length, table, c.cache, out, ws, 1.0, groups=ints([0, 2])),
+        lambda: B.sjd_page_attention(c.pages, q, start, length, table, c.cache, out, ws, 0.0),
+        lambda: B.sjd_page_attention(c.pages, q[:, :100], start, length, table, c.cache, out[:, :100], ws, 1.0),
+        lambda: B.sjd_page_append(c.pages, k, k[:, ::2], start, length, table, c.cache),
+        lambda: B.sjd_page_append(c.pages, q, q, start, length, table, c.cache),
+        lambda: B.sjd_page_append(c.pages, k, k, start, length, table, c.cache, q=q),
+        lambda: B.sjd_page_append(c.pages, k, k, start, length, table, c.cache, q=q, q_out=out),
+        lambda: B.sjd_page_append(c.pages, k, k, start, length, table, c.cache, turns=t.int()),
+        lambda: B.sjd_page_append(c.pages, k, k, start.long(), length, table, c.cache),
+        lambda: B.sjd_rope(q, out, start, 64, t),
+        lambda: B.sjd_rope(q, out, ints([1, 2, 3, 4]), 48, t),
+        lambda: B.sjd_rope(q, out, ints([1, 2, 3, 4]), 64, torch.zeros(33, dtype=torch.int64, device="cuda")),
+        lambda: B.sjd_block_norm(q, torch.zeros(4, 256, device="cuda"), 1e-5, out),
+        lambda: B.sjd_block_norm(q, torch.zeros(4, 256, device="cuda").bfloat16(), 1e-5),
+        lambda: B.sjd_block_norm(q, torch.zeros(4, 256, device="cuda"), 1e-5, gate=k),
+        lambda: B.sjd_block_norm(q, torch.zeros(4, 256, device="cuda"), -1.0),
+    ]
+    for f in bad:
+        with pytest.raises(B.SjdError) as e:
+            f()
+        assert e.value.code == B.SJD_EINVAL
+    torch.cuda.synchronize()
