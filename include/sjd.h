@@ -467,11 +467,12 @@ int sjd_page_append(const sjd_pages *pages, const void *q, int64_t ldq, int32_t 
 /* Attention of the new tokens' queries q dev [rows x n_heads * head_dim] (as they are: turned already) over the pages, the tokens' own keys included:
  * softmax(scale q k) v -> out, like q, rows of length ldo.  The query at position p sees the positions j <= p with, if window > 0, also j > p - window or j < sinks; one
  * that sees nothing gives zeros.  Query head h reads cache head h / (n_heads / n_kv_heads).
- * Groups: the sequences groups[g] .. groups[g + 1] - 1 (groups dev int32 [n_groups + 1], ascending) begin with the same prefix[g] positions (dev int32 [n_groups]) in
- * the same pages, say images of one prompt: what whole records of 32 positions of it hold is read and weighed once for all of them.  It may be claimed only where
- * their table rows do name the same pages that far.  The result does not depend on it but for the order of sums.  n_groups 0: none.  With window > 0 groups are not used.
- * scale is finite and above zero.  Scores and sums are fp32, bf16 probabilities have at least 8 bits; scores that overflow give NaN, as does a visible infinity or NaN among the
- * values.  What masked positions hold, NaN included, does not reach `out`.  workspace: sjd_page_attention_workspace bytes (may be 0), 16-byte aligned.
+ * Groups: the sequences groups[g] .. groups[g + 1] - 1 (groups dev int32 [n_groups + 1], ascending) begin with the same prefix[g] positions (dev int32 [n_groups]), say
+ * images of one prompt, and their table rows name the same pages for the whole pages of it, prefix[g] / page of them: those are read and weighed once for all.
+ * (What is left of the prefix lies in pages that each sequence goes on in, so in copies.)  The result does not depend on it but for the order of sums.  n_groups 0:
+ * none.  With window > 0 groups are not used.
+ * scale is finite and above zero.  Scores and sums are fp32, bf16 probabilities have at least 8 bits.  Scores that overflow give NaN; a visible infinity or NaN among the values
+ * gives an infinity or NaN in that dimension.  What masked positions hold, NaN included, does not reach `out`.  workspace: sjd_page_attention_workspace bytes (may be 0), 16-byte aligned.
  * rows <= 2^24, n_seqs <= 65535, heads <= 4096.                                                  */
 int sjd_page_attention_workspace(const sjd_pages *pages, int32_t rows, int32_t n_seqs, int32_t n_groups, int32_t n_heads, int32_t width, size_t *bytes);
 int sjd_page_attention(const sjd_pages *pages, const void *q, int64_t ldq, int32_t n_heads, int32_t rows, const int32_t *start, const int32_t *len, int32_t n_seqs,

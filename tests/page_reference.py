@@ -89,22 +89,17 @@ def attention(cache, q, start, length, table, page, scale, bf16, window=0, sinks
         if not fits(n, m, table.shape[1], page) or m == 0:
             continue
         k, v, held = sequence(cache, table[b], page, n + m, bf16)
-        g = heads // k.shape[1]
-        j = np.arange(n + m)
-        for i in range(m):
-            p = n + i
-            see = held & (j <= p) & ((j > p - window) | (j < sinks) if window else True)
-            for h in range(heads):
-                ks, vs = k[see][:, h // g], v[see][:, h // g]
-                r = start[b] + i
-                if not len(ks):
-                    out[r, h], mag[r, h], top[r, h] = 0, 0, 0
-                    continue
-                s = ks @ q[r, h] * scale
-                w = np.exp(s - s.max())
-                out[r, h] = w @ vs / w.sum()
-                mag[r, h] = (np.abs(ks) @ np.abs(q[r, h])).max() * scale
-                top[r, h] = np.abs(vs).max()
+        g, r = heads // k.shape[1], slice(start[b], start[b + 1])
+        j, p = np.arange(n + m)[None], np.arange(n, n + m)[:, None]
+        see = held[None] & (j <= p) & ((j > p - window) | (j < sinks) if window else True)
+        some = see.any(-1)
+        for h in range(heads):
+            ks, vs = k[:, h // g], v[:, h // g]
+            s = np.where(see, q[r, h] @ ks.T * scale, -np.inf)
+            w = np.exp(s - np.where(some, s.max(-1), 0)[:, None])
+            out[r, h] = np.where(some[:, None], w @ vs / np.maximum(w.sum(-1), 1e-300)[:, None], 0)
+            mag[r, h] = np.where(see, np.abs(q[r, h]) @ np.abs(ks).T, 0).max(-1) * scale
+            top[r, h] = np.where(see, np.abs(vs).max(-1)[None], 0).max(-1)
     return out, mag, top
 
 

@@ -232,12 +232,12 @@ def test_attention_over_long_and_cut_walks(B, length, tokens, heads, kv, window,
     (8, [64, 100, 65], [1, 4, 1], [0, 3], [64]), (8, [100, 31], [1, 1], [0, 2], [31]), (8, [64, 33, 70], [9, 2, 9], [0, 2], [32]), (32, [500, 500], [1, 1], [0, 1], [500]),
     (32, [500, -1, 640, 2000], [2, 2, 2, 60], [0, 4], [480]), (32, [-1, 500, 640], [2, 2, 2], [0, 3], [480]), (32, [0, 0], [200, 170], [0, 2], [128]), (32, [448, 448, 449], [30, 100, 1], [0, 3], [448])])
 def test_a_shared_prefix(B, width, length, tokens, groups, prefix, hd, page, dtype):
-    """as without groups; the first prefix[g] positions of a group lie in the same pages"""
+    """as without groups; the whole pages of the first prefix[g] positions of a group are the same"""
     width = width * 64 // page
     c = Paged(B, len(length), 2, hd, page, width, dtype)
     for g, p in enumerate(prefix):
         c.table[groups[g]:groups[g + 1], :p // page] = c.table[groups[g], :p // page]
-        if p % page:                                            # (a page of which whole records are shared, the rest is each one's own: copied)
+        if p % page:                                            # (the rest of the prefix is in copies)
             for b in range(groups[g] + 1, groups[g + 1]):
                 c.cache[c.table[b, p // page], :, :p % page // 32] = c.cache[c.table[groups[g], p // page], :, :p % page // 32]
     c.ref = host(c.cache)
@@ -246,6 +246,58 @@ def test_a_shared_prefix(B, width, length, tokens, groups, prefix, hd, page, dty
     if any(R.fits(n, m, width, page) for n, m in zip(length, tokens)):
         two = c.check(length, tokens, 8)
         assert np.abs(np.nan_to_num(one) - np.nan_to_num(two)).max() < (0.1 if dtype == "bf16" else 1e-4)
+
+
+@pytest.mark.parametrize("hd", [32, 64, 96, 128])
+@pytest.mark.parametrize("length,tokens,kw", [([0, 64, 33], [300, 129, 200], {}), ([300, 0], [260, 400], dict(window=70, sinks=40)), ([31], [640], dict(pad=3)),
+                                              ([448, 450, 460], [240, 100, 300], dict(groups=[0, 3], prefix=[448])), ([0, 10], [350, 330], dict(groups=[0, 2], prefix=[128])),
+                                              ([64, 64, -1, 64, 0], [130, 128, 9, 150, 200], dict(groups=[0, 4], prefix=[64], behind=5))])
+def test_tiles_of_many_rows(B, length, tokens, kw, hd):
+    c = Paged(B, len(length), 8, hd, 32, 26, "bf16")
+    if "prefix" in kw:
+        p = kw["prefix"][0] // 32
+        c.table[:kw["groups"][1], :p] = c.table[0, :p]
+    c.table[0, 1] = c.table[0, 1] if "prefix" in kw else -1                 # a page that is not the pool's
+    assert (sum(tokens) * 8 >> 7) * 8 >= 256
+    c.check(length, tokens, 64, **kw)
+
+
+def test_masked_values_of_many_rows(B):
+    """NaN and infinities that masks hide from some rows of a tile and not from others"""
+    c = Paged(B, 2, 8, 128, 64, 12, "bf16")
+    length, tokens = [20, 300], [320, 330]
+    clean = c.check(length, tokens, 64)
+    _, v = R.record_at(128, True)
+    for b, p, d, x in ((0, 150, 7, float("nan")), (0, 339, 100, float("inf")), (1, 301, 0, float("-inf")), (1, 629, 64, float("nan"))):
+        c.cache[c.table[b, p // 64], :, p % 64 // 32, int(v[p % 32, d])] = x
+    rest = c.cache[c.table[1, 630 // 64], :, 630 % 64 // 32]                # the rest of the last record
+    rest[:, torch.from_numpy(v[630 % 32:].reshape(-1)).cuda()] = float("nan")
+    got, *_ = c.attend(length, tokens, 64)
+    want = clean.copy()
+    for row, d in ((130, 7), (319, 100), (320 + 1, 0), (320 + 329, 64)):
+        last = 320 if row < 320 else 650
+        want[row:last, :, d] = np.nan
+    # (the formula gives an infinity where one is seen, or NaN: by both, a value that is not finite)
+    assert np.array_equal(np.isfinite(got), np.isfinite(want)) and np.array_equal(got[np.isfinite(want)], want[np.isfinite(want)])
+    assert np.isnan(got[130:320, :, 7]).all() and np.isnan(got[649, :, 64]).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n_seqs,width", [(61, 4), (70, 40), (150, 40)])
+def test_more_sequences_than_lanes(B, n_seqs, width, dtype):
+    rng = np.random.RandomState(n_seqs)
+    c = Paged(B, n_seqs, 1, 64, 32, width, dtype)
+    groups = [3, 20, 21, 50, n_seqs]
+    prefix = [100, 64, 96, 33]
+    length = [int(x) for x in rng.randint(100, 110 if width == 4 else 1200, n_seqs)]
+    tokens = [int(x) for x in rng.randint(0, 4, n_seqs)]
+    length[5] = length[n_seqs - 1] = -1
+    for g, p in enumerate(prefix):
+        c.table[groups[g]:groups[g + 1], :p // 32] = c.table[groups[g], :p // 32]
+    c.check(length, tokens, 6, groups=groups, prefix=prefix, behind=1)
+    c.check(length, tokens, 6, behind=1)
+    c.table = np.random.RandomState(1).permutation(c.n_pages)[:n_seqs * width].reshape(n_seqs, width).astype(np.int32)
+    c.append(length, tokens, heads=2, t=B.sjd_rope_turns(10000.0, 64))
 
 
 def test_groups_and_starts_of_no_sense_stay_inside(B):
