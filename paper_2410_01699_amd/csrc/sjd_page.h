@@ -30,6 +30,18 @@ __device__ __forceinline__ int64_t page_record(const PageSeqs &sq, const int32_t
     return (uint32_t)id < (uint32_t)sq.n_pages ? (((int64_t)id * heads + head) << sh) + (blk & ((1 << sh) - 1)) : -1;
 }
 
+__device__ __forceinline__ int page_lane(int x, int l) { return __builtin_amdgcn_readlane(x, l); }
+// The sum over this lane and those before it: inside rows of 16 lanes, then from row to row
+template <int CTRL, int ROWS> __device__ __forceinline__ int page_from(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false); }
+template <int CTRL, int ROWS> __device__ __forceinline__ float page_from(float x) { return __int_as_float(page_from<CTRL, ROWS>(__float_as_int(x))); }
+template <typename N> __device__ __forceinline__ N page_sum_up(N x)
+{
+    x += page_from<0x111, 0xF>(x); x += page_from<0x112, 0xF>(x); x += page_from<0x114, 0xF>(x); x += page_from<0x118, 0xF>(x);
+    x += page_from<0x142, 0xA>(x);
+    x += page_from<0x143, 0xC>(x);
+    return x;
+}
+
 static inline bool page_shape(const sjd_pages *p)
 {
     if (!p || (p->dtype != 0 && p->dtype != 1) || p->n_kv_heads < 1 || p->n_kv_heads > PAGE_MAX_HEADS || p->n_pages < 1) return false;
@@ -51,15 +63,18 @@ static inline bool page_seqs(const sjd_pages *p, const int32_t *start, const int
 // series of sine and cosine, whose first terms left out are r^11 / 11! < 2e-9 and r^12 / 12! < 2e-10.
 __device__ __forceinline__ void rope_angle(int pos, uint64_t turns, float magnitude, float &c, float &s)
 {
-    const uint64_t a = (uint64_t)(int64_t)pos * turns + 0x2000000000000000ull;         // (an eighth up, so that the top two bits round)
-    const int quarter = (int)(a >> 62);
-    const float r = (float)((int)((uint32_t)(a >> 32) & 0x3FFFFFFFu) - 0x20000000) * 1.4629180792671596e-9f;        // 2 pi / 2^32
+    // the product's upper half, an eighth up, so that its top two bits round (a negative position is 2^32 too large where it is multiplied)
+    const uint32_t p = (uint32_t)pos, lo = (uint32_t)turns, hi = (uint32_t)(turns >> 32);
+    const uint32_t a = __umulhi(p, lo) + p * hi - (pos < 0 ? lo : 0u) + 0x20000000u;
+    const int quarter = (int)(a >> 30);
+    const float r = (float)((int)(a & 0x3FFFFFFFu) - 0x20000000) * 1.4629180792671596e-9f;        // 2 pi / 2^32
     const float z = r * r;
     const float sn = r * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -0.16666667f), 1.f);
     const float cn = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.f);
     const float cs = (quarter & 1) ? sn : cn, ss = (quarter & 1) ? cn : sn;
-    c = (quarter == 1 || quarter == 2) ? -cs * magnitude : cs * magnitude;
-    s = (quarter & 2) ? -ss * magnitude : ss * magnitude;
+    // cosines are negative in quarters 1 and 2, sines in 2 and 3
+    c = __uint_as_float(__float_as_uint(cs) ^ ((a + 0x40000000u) & 0x80000000u)) * magnitude;
+    s = __uint_as_float(__float_as_uint(ss) ^ (a & 0x80000000u)) * magnitude;
 }
 struct Rope { const uint64_t *turns; int32_t rot, interleaved; float magnitude, sign; };      // rot 0: nothing turns
 // (the fields of a call, or nothing to turn)
@@ -83,7 +98,13 @@ __device__ __forceinline__ void eight_set(Eight<float> &x, const float (&v)[8])
     x.w[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
     x.w[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
 }
-__device__ __forceinline__ uint32_t bf16_pair(float a, float b) { return (uint32_t)f32_to_bf16(a) | (uint32_t)f32_to_bf16(b) << 16; }
+// Two values in bf16, to the nearest, ties to even, NaN stays NaN: one instruction
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b)
+{
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    typedef __attribute__((ext_vector_type(2))) __bf16 b16x2;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, b16x2));
+}
 __device__ __forceinline__ void eight_set(Eight<bf16_t> &x, const float (&v)[8])
 {
     x.w[0] = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
@@ -105,7 +126,7 @@ template <> __device__ __forceinline__ float one_get<float>(float v) { return v;
 template <> __device__ __forceinline__ float one_get<bf16_t>(bf16_t v) { return bf16_to_f32(v); }
 template <typename T> __device__ __forceinline__ T one_set(float v);
 template <> __device__ __forceinline__ float one_set<float>(float v) { return v; }
-template <> __device__ __forceinline__ bf16_t one_set<bf16_t>(float v) { return f32_to_bf16(v); }
+template <> __device__ __forceinline__ bf16_t one_set<bf16_t>(float v) { return (bf16_t)bf16_pair(v, v); }
 
 // Unit u of a head's hd / 16: sixteen values in two eights, at eight_at(u, 0) and eight_at(u, 1).  Where rot is a multiple of 16 the first
 // rot / 16 units hold both values of their pairs: the eights u and u + rot / 16 of the half layout, two neighbours of the interleaved one.

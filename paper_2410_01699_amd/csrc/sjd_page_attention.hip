@@ -80,7 +80,6 @@ __device__ __forceinline__ PaSeg pa_segment(const PaPlan &pl, int s)
     pa_blocks(pl, sg, g, g < 0 ? 0 : pa_shared(pl, g));
     return sg;
 }
-__device__ __forceinline__ int pa_lane(int x, int l) { return __builtin_amdgcn_readlane(x, l); }
 // Segment `lane` of the first 64.  Where these are all, everything is requested at once and goes from lane to lane: a trip to memory costs more than all that
 // follows it.
 __device__ __forceinline__ PaSeg pa_first(const PaPlan &pl, int lane)
@@ -101,9 +100,9 @@ __device__ __forceinline__ PaSeg pa_first(const PaPlan &pl, int lane)
     int g = -1, shared = ge - gs < 2 ? 0 : min(max(pre, 0) >> pl.sq.page_shift, pl.sq.width) << (pl.sq.page_shift - 5);
     int mine = 0;
     for (int i = pl.n_groups - 1; i >= 0; --i) {            // (the first group that has the sequence)
-        const int lo = pa_lane(gs, i), hi = pa_lane(ge, i), sh = pa_lane(shared, i);
+        const int lo = page_lane(gs, i), hi = page_lane(ge, i), sh = page_lane(shared, i);
         if (b >= lo && b < hi) { g = i; mine = sh; }
-        const int f = pa_lane(sg.r0, min(pl.n_groups + lo, 63)), l = pa_lane(r1, max(min(pl.n_groups + hi, 64) - 1, 0));
+        const int f = page_lane(sg.r0, min(pl.n_groups + lo, 63)), l = page_lane(r1, max(min(pl.n_groups + hi, 64) - 1, 0));
         if (lane == i && shared) { sg.r0 = f; sg.m = max(l - f, 0); sg.n = 0; sg.seq = sg.front = lo; sg.first = hi - lo; sg.count = sg.m ? shared : 0; }
     }
     if (b < 0 && !shared) sg.m = 0;
@@ -114,16 +113,6 @@ __device__ __forceinline__ int pa_tiles(const PaPlan &pl, const PaSeg &sg) { ret
 
 // What a slot is: its segment, tile and split, the first slot of the segment, and of own segments the number of its first tile among the own ones
 struct PaPart { PaSeg sg; int32_t seg, tile, split, splits, per, base, own; };
-// The sum over this lane and those before it: inside rows of 16 lanes, then from row to row
-template <int CTRL, int ROWS> __device__ __forceinline__ int pa_from(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false); }
-template <int CTRL, int ROWS> __device__ __forceinline__ float pa_from(float x) { return __int_as_float(pa_from<CTRL, ROWS>(__float_as_int(x))); }
-template <typename N> __device__ __forceinline__ N pa_sum_up(N x)
-{
-    x += pa_from<0x111, 0xF>(x); x += pa_from<0x112, 0xF>(x); x += pa_from<0x114, 0xF>(x); x += pa_from<0x118, 0xF>(x);
-    x += pa_from<0x142, 0xA>(x);
-    x += pa_from<0x143, 0xC>(x);
-    return x;
-}
 // Lanes look at 64 segments at a time, c0: those of the first 64.  by_seg: the first slot of the given segment.  own_total: all own tiles, if it is found in
 // the walk's last 64.  With per >= total / slots the splits of all tiles are at most slots + tiles.
 __device__ __forceinline__ bool pa_part(const PaPlan &pl, const PaSeg &c0, int per, int want, bool by_seg, PaPart &part, int &own_total)
@@ -135,23 +124,23 @@ __device__ __forceinline__ bool pa_part(const PaPlan &pl, const PaSeg &c0, int p
         const bool prefix = s0 + lane < pl.n_groups;
         const int splits = max((int)(((int64_t)sg.count + per - 1) / per), !prefix && sg.m ? 1 : 0);     // (of own segments one at least, which may be empty)
         const int tiles = splits ? pa_tiles(pl, sg) : 0, mine = tiles * splits, mine_own = prefix ? 0 : tiles;
-        const int incl = pa_sum_up(mine), incl_own = pa_sum_up(mine_own), begin = base + incl - mine;
+        const int incl = page_sum_up(mine), incl_own = page_sum_up(mine_own), begin = base + incl - mine;
         const uint64_t hit = by_seg ? __ballot(s0 + lane == want) : __ballot(want >= begin && want < begin + mine);
-        own_total = own + pa_lane(incl_own, 63);
+        own_total = own + page_lane(incl_own, 63);
         if (hit) {
             const int l = __ffsll((unsigned long long)hit) - 1;
-            part.sg = {pa_lane(sg.r0, l), pa_lane(sg.m, l), pa_lane(sg.n, l), pa_lane(sg.seq, l), pa_lane(sg.g, l), pa_lane(sg.first, l), pa_lane(sg.front, l), pa_lane(sg.count, l)};
+            part.sg = {page_lane(sg.r0, l), page_lane(sg.m, l), page_lane(sg.n, l), page_lane(sg.seq, l), page_lane(sg.g, l), page_lane(sg.first, l), page_lane(sg.front, l), page_lane(sg.count, l)};
             part.seg = s0 + l;
-            part.splits = pa_lane(splits, l);
-            part.base = pa_lane(begin, l);
-            part.own = own + pa_lane(incl_own - mine_own, l);
+            part.splits = page_lane(splits, l);
+            part.base = page_lane(begin, l);
+            part.own = own + page_lane(incl_own - mine_own, l);
             part.per = per;
             const int at = by_seg ? 0 : want - part.base, d = max(part.splits, 1);
             part.tile = at / d;
             part.split = at - part.tile * d;
             return true;
         }
-        base += pa_lane(incl, 63);
+        base += page_lane(incl, 63);
         own = own_total;
     }
     return false;
@@ -163,8 +152,8 @@ __device__ __forceinline__ int pa_per(const PaPlan &pl, const PaSeg &c0)
     float total = 0.f;
     for (int s0 = 0; s0 < n; s0 += 64) {
         const PaSeg sg = s0 == 0 ? c0 : s0 + lane < n ? pa_segment(pl, s0 + lane) : PaSeg{};
-        const float c = pa_sum_up((float)sg.count * pa_tiles(pl, sg));
-        total += __int_as_float(pa_lane(__float_as_int(c), 63));
+        const float c = page_sum_up((float)sg.count * pa_tiles(pl, sg));
+        total += __int_as_float(page_lane(__float_as_int(c), 63));
     }
     return (int)fmaxf((float)pl.least, fminf(ceilf(total / (float)pl.slots), 1e9f));
 }
@@ -247,14 +236,6 @@ __device__ __forceinline__ uint32_t pa_wild(uint32_t w, float) { return ((w & 0x
 // record of a part: O[rows][hd], then m and l of the rows
 __device__ __forceinline__ size_t pa_record(int rows, int hd) { return (size_t)rows * (hd + 2); }
 
-// Two values in bf16
-__device__ __forceinline__ uint32_t pa_b16(float a, float b)
-{
-    typedef __attribute__((ext_vector_type(2))) float f32x2;
-    typedef __attribute__((ext_vector_type(2))) __bf16 b16x2;
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, b16x2));
-}
-
 template <typename T> __device__ __forceinline__ void pa_out(T *p, const f32x4 &v, bool vec);
 template <> __device__ __forceinline__ void pa_out<float>(float *p, const f32x4 &v, bool vec)
 {
@@ -263,8 +244,8 @@ template <> __device__ __forceinline__ void pa_out<float>(float *p, const f32x4 
 }
 template <> __device__ __forceinline__ void pa_out<bf16_t>(bf16_t *p, const f32x4 &v, bool vec)
 {
-    if (vec) *reinterpret_cast<uint2 *>(p) = make_uint2(pa_b16(v[0], v[1]), pa_b16(v[2], v[3]));
-    else { p[0] = f32_to_bf16(v[0]); p[1] = f32_to_bf16(v[1]); p[2] = f32_to_bf16(v[2]); p[3] = f32_to_bf16(v[3]); }
+    if (vec) *reinterpret_cast<uint2 *>(p) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+    else { p[0] = one_set<bf16_t>(v[0]); p[1] = one_set<bf16_t>(v[1]); p[2] = one_set<bf16_t>(v[2]); p[3] = one_set<bf16_t>(v[3]); }
 }
 
 // What a workgroup is about.  own: a sequence's own positions; alone: the only part of its rows; [gs, ge): a group's sequences; entries e0 .. of the segment's, each a
@@ -379,9 +360,9 @@ __device__ __forceinline__ void pa_pack(const float (&x)[8], bool coarse, uint4 
 {
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        const uint32_t h = pa_b16(x[2 * w], x[2 * w + 1]);
+        const uint32_t h = bf16_pair(x[2 * w], x[2 * w + 1]);
         (&hi.x)[w] = h;
-        if (!coarse) (&lo.x)[w] = pa_b16(x[2 * w] - __uint_as_float(h << 16), x[2 * w + 1] - __uint_as_float(h & 0xFFFF0000u));
+        if (!coarse) (&lo.x)[w] = bf16_pair(x[2 * w] - __uint_as_float(h << 16), x[2 * w + 1] - __uint_as_float(h & 0xFFFF0000u));
     }
 }
 // Zero times NaN is NaN: where a mask may hide an infinity or NaN from some row it is taken out of the values, and the rows that see one are counted.
