@@ -43,9 +43,10 @@ __device__ __forceinline__ int pa_group_of(const PaPlan &pl, int b)         // t
     return lo > 0 && b < pl.groups[lo] ? lo - 1 : -1;
 }
 // Blocks of the whole pages that the sequences of group g have in common, 0 where the group has fewer than two
+__device__ __forceinline__ int pa_inside(const PaPlan &pl, int b) { return min(max(b, 0), pl.sq.n_seqs); }
 __device__ __forceinline__ int pa_shared(const PaPlan &pl, int g)
 {
-    const int gs = max(pl.groups[g], 0), ge = min(pl.groups[g + 1], pl.sq.n_seqs);
+    const int gs = pa_inside(pl, pl.groups[g]), ge = pa_inside(pl, pl.groups[g + 1]);
     if (ge - gs < 2) return 0;
     return min(max(pl.prefix[g], 0) >> pl.sq.page_shift, pl.sq.width) << (pl.sq.page_shift - 5);
 }
@@ -65,7 +66,7 @@ __device__ __forceinline__ PaSeg pa_segment(const PaPlan &pl, int s)
 {
     PaSeg sg = {0, 0, 0, 0, -1, 0, 0, 0};
     if (s < pl.n_groups) {
-        const int shared = pa_shared(pl, s), gs = max(pl.groups[s], 0), ge = min(pl.groups[s + 1], pl.sq.n_seqs);
+        const int shared = pa_shared(pl, s), gs = pa_inside(pl, pl.groups[s]), ge = pa_inside(pl, pl.groups[s + 1]);
         if (!shared) return sg;
         sg.r0 = min(max(pl.sq.start[gs], 0), pl.sq.rows);
         sg.m = min(max(pl.sq.start[ge], sg.r0), pl.sq.rows) - sg.r0;
@@ -91,7 +92,7 @@ __device__ __forceinline__ PaSeg pa_first(const PaPlan &pl, int lane)
     int gs = 0, ge = 0, pre = 0, s0 = 0, s1 = 0;
     if (lane < pl.n_groups) { gs = pl.groups[lane]; ge = pl.groups[lane + 1]; pre = pl.prefix[lane]; }
     if (b >= 0 && lane < n) { s0 = pl.sq.start[b]; s1 = pl.sq.start[b + 1]; sg.n = pl.sq.len[b]; }
-    gs = max(gs, 0); ge = min(ge, pl.sq.n_seqs);
+    gs = pa_inside(pl, gs); ge = pa_inside(pl, ge);
     sg.r0 = min(max(s0, 0), pl.sq.rows);
     const int r1 = min(max(s1, sg.r0), pl.sq.rows);
     sg.m = r1 - sg.r0;
@@ -437,7 +438,7 @@ template <typename T, int KS> __device__ __forceinline__ void pa_query(const T *
 // two bf16 (16 bits), which costs nothing where memory bounds.
 // Up to 32 rows: a workgroup has 16 MT; its waves take the blocks in turn, each for all rows, so that a record goes straight to the registers of one wave.
 template <int HD, typename T, int MT>
-__global__ __launch_bounds__(64 * PA_WAVES, HD * (int)sizeof(T) * (MT + 3) <= 1280 ? 2 : 1) void page_few_kernel(const T *__restrict__ q, int64_t ldq,
+__global__ __launch_bounds__(64 * PA_WAVES, HD <= 128 && HD * (int)sizeof(T) * MT <= 512 ? 2 : 1) void page_few_kernel(const T *__restrict__ q, int64_t ldq,
                                                                                                        const T *__restrict__ cache, PaPlan pl, float qk, T *__restrict__ out,
                                                                                                        int64_t ldo, int vec, float *__restrict__ part)
 {
@@ -857,9 +858,11 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void page_many_kernel(const bf16_
         const bool edge = pl.window || block(n, NB - 1) * 32 + 31 > first || (holds >> (NB * (n & 1)) & 3u) != 3u;
         if (edge) clean(n, now);
         work(n, now, edge);
-        __syncthreads();                        // (loads into LDS are waited for as well)
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // the loads into LDS
+        __syncthreads();
     };
     if (steps) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         for (int n = 0; n < steps; n += 2) {
             step(n, even, odd);
@@ -957,7 +960,7 @@ static int pa_plan(const sjd_pages *p, int rows, int n_seqs, int n_groups, int n
     const int64_t own = (entries >> pl->rows_shift) + n_seqs, shared = n_groups ? (entries >> pl->rows_shift) + n_groups : 0;
     const int64_t nblk = ((int64_t)width * p->page + 31) / 32;
     const bool few = own * p->n_kv_heads < (mean > 64 ? 320 : 512);
-    const int resident = row > 256 ? 256 : row > 128 && pl->rows_shift == 5 ? 384 : 512;
+    const int resident = row > 512 || p->head_dim > 128 || (row > 256 && pl->rows_shift == 5) ? 256 : row > 128 && pl->rows_shift == 5 ? 384 : 512;
     pl->slots = nblk <= 32 || !few ? 0 : std::max(1, resident / p->n_kv_heads);
     pl->least = 2 * PA_WAVES;
     pl->n_groups = n_groups;
@@ -1038,8 +1041,9 @@ extern "C" int sjd_page_attention(const sjd_pages *pages, const void *q, int64_t
     if (join) {
         // (workgroups for tiles as full as they are on average: many hold one token)
         const int64_t full = std::min<int64_t>((int64_t)1 << pl.rows_shift, ((int64_t)rows * pl.group + n_seqs - 1) / n_seqs);
-        const int chunks = (int)((full * (hd / 4) + PA_UNITS - 1) / PA_UNITS);
-        const dim3 mgrid((unsigned)((int64_t)pl.tiles * chunks * pl.heads));
+        const int64_t tiles = (int64_t)pl.tiles * pl.heads;
+        const int chunks = (int)std::min((full * (hd / 4) + PA_UNITS - 1) / PA_UNITS, std::max<int64_t>(1, ((int64_t)1 << 23) / tiles));
+        const dim3 mgrid((unsigned)(tiles * chunks));
         if (dt == 0) SJD_LAUNCH((page_merge_kernel<float>), mgrid, dim3(PA_UNITS * PA_JOIN), 0, s, (const float *)ws, pl, hd, chunks, (float *)out, ldo, vec);
         else SJD_LAUNCH((page_merge_kernel<bf16_t>), mgrid, dim3(PA_UNITS * PA_JOIN), 0, s, (const float *)ws, pl, hd, chunks, (bf16_t *)out, ldo, vec);
         HIP_TRY(hipGetLastError());
