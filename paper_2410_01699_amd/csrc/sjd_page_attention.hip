@@ -757,12 +757,9 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void page_many_kernel(const bf16_
                     s[mt][2 * i + 1] = P::score(ka[ks][1], qa[mt][ks], s[mt][2 * i + 1]);
                 }
         }
-        // the first block's values are read while the weights are made, the second's during the first's products
-        __builtin_amdgcn_sched_barrier(0);
-        uint4 va[DT];
+        uint4 va[DT];                           // of the first block; the second's are read during the first's products
 #pragma unroll
         for (int t = 0; t < DT; ++t) va[t] = *reinterpret_cast<const uint4 *>(buf + vat + P::v_at(t, 0));
-        __builtin_amdgcn_sched_barrier(0);
         const int last = k0[NB - 1] + 31;
         const bool whole = held == 3u && __ballot(!(last <= low)) == 0 && (pl.window == 0 || last < pl.sinks || (wk.own && k0[0] > high - pl.window));
         if (edge) {
@@ -828,7 +825,9 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void page_many_kernel(const bf16_
                 }
             }
         }
-        // no branches from here on: a block's weights are made while the products of the one before run
+        // No branches from here on: a block's weights are made while the products of the one before run.  This part goes before the other workgroup's loads and
+        // scores on the same CU: 144 us against 153, 4000 tokens of 32 heads of 128.
+        __builtin_amdgcn_s_setprio(1);
         const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
@@ -849,6 +848,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void page_many_kernel(const bf16_
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) o[mt][DT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_b16(ones), as_b16(ph[mt]), o[mt][DT], 0, 0, 0);
         }
+        __builtin_amdgcn_s_setprio(0);
     };
     auto step = [&](int n, uint8_t *now, uint8_t *next) {
         if (n + 1 < steps) {
