@@ -2,7 +2,8 @@
 #include "sjd_page.h"
 
 // A row to a workgroup, in registers from the first sum to the last: thread t has the eights t, t + 256, ...  (NE of them), zeros behind the row.
-// Two sums over the row, of x^2 and of h^2, each over a wave's lanes and then over the waves through LDS.
+// Two sums over the row, of x^2 and of h^2, each over a wave's lanes and then over the waves through LDS.  Memory bounds: 2048 rows of 4096, a gate a row, bf16
+// 22.1 us, 117 MB at a copy's 5.1 TB/s (resid partly stays in the memory-side cache); one row 4.1 us, launch and the two sums.
 #define BN_THREADS 256
 __device__ __forceinline__ float bn_sum(float v, float *red)
 {

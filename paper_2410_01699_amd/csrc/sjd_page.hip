@@ -27,7 +27,8 @@ extern "C" int sjd_rope_turns(double theta, int32_t rot_dim, int32_t scaling, do
 }
 
 // ---- rotation of rows ---------------------------------------------------------------------------
-// A thread turns one unit (sixteen values, eight pairs) of NH heads of a row: the angles are the heads' own, so they are made once.
+// A thread turns one unit (sixteen values, eight pairs) of NH heads of a row: angles are the same for all heads, so they are made once.  Memory bounds: 4001 rows of
+// 40 heads of 128, 64 dimensions turned, bf16 16 us, 82 MB at a copy's 5.1 TB/s; one row 2.6 us, launch and latency.
 template <typename T, int NH>
 __global__ __launch_bounds__(256) void rope_kernel(const T *x, int64_t ldx, T *out, int64_t ldo, const int32_t *__restrict__ pos, uint32_t rows,
                                                    uint32_t heads, uint32_t hd, Rope ro)
@@ -137,6 +138,8 @@ __device__ __forceinline__ bool page_item(const PageSeqs &sq, int want, PageItem
 
 // A workgroup takes the new rows of one block of a sequence: of one cache head its keys (turned) and values, through LDS into the record's order,
 // or of NH query heads the turned rows.  vec: rows of 16-byte units whose pairs lie in units; else values one by one.
+// 4791 rows of prompts, 32/8 heads of 128, bf16: 27 us, 118 MB at 4.4 TB/s (a copy: 5.1); a workgroup loads, turns and stores one after the other.  Windows of 16 for 8
+// sequences, 32 heads, fp32: 7 us, four trips to memory in a row (lengths, page, rows, records).
 template <int HD, typename T, int NH>
 __global__ __launch_bounds__(256) void page_append_kernel(PageSeqs sq, const T *q, int64_t ldq, T *q_out, int64_t ldqo, const T *__restrict__ k,
                                                           const T *__restrict__ v, int64_t ld, int heads, int kv, int sets, Rope ro, int vec, T *__restrict__ cache)

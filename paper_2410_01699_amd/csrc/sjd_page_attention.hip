@@ -356,14 +356,14 @@ __device__ __forceinline__ void pa_weights(const PaPlan &pl, const f32x4 (&s)[2]
 #pragma unroll
     for (int e = 0; e < 8; ++e) l += x[e];
 }
-// Weights as the second product's operand: two bf16 (16 bits) or, coarse, one
-__device__ __forceinline__ void pa_pack(const float (&x)[8], bool coarse, uint4 &hi, uint4 &lo)
+// Weights as the second product's operand, two bf16: 16 bits
+__device__ __forceinline__ void pa_pack(const float (&x)[8], uint4 &hi, uint4 &lo)
 {
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         const uint32_t h = bf16_pair(x[2 * w], x[2 * w + 1]);
         (&hi.x)[w] = h;
-        if (!coarse) (&lo.x)[w] = bf16_pair(x[2 * w] - __uint_as_float(h << 16), x[2 * w + 1] - __uint_as_float(h & 0xFFFF0000u));
+        (&lo.x)[w] = bf16_pair(x[2 * w] - __uint_as_float(h << 16), x[2 * w + 1] - __uint_as_float(h & 0xFFFF0000u));
     }
 }
 // Zero times NaN is NaN: where a mask may hide an infinity or NaN from some row it is taken out of the values, and the rows that see one are counted.
@@ -437,6 +437,8 @@ template <typename T, int KS> __device__ __forceinline__ void pa_query(const T *
 // above that, a block costs 8 exponentials a lane and tile, their sum and a comparison beside its products.  bf16: probabilities go in as
 // two bf16 (16 bits), which costs nothing where memory bounds.
 // Up to 32 rows: a workgroup has 16 MT; its waves take the blocks in turn, each for all rows, so that a record goes straight to the registers of one wave.
+// Memory bounds: 6.9 TB/s with every CU at it (8 x 16 queries of 32 heads of 128, fp32: 1 MB a workgroup in 37 us), but a workgroup's cut takes 2 us, its first records
+// 2 to 3, its waves' sums 1 to 3: 29 us for 134 MB (one query, 4 k positions), 23 for 79 (16 queries behind a prefix of 14 k).
 template <int HD, typename T, int MT>
 __global__ __launch_bounds__(64 * PA_WAVES, HD <= 128 && HD * (int)sizeof(T) * MT <= 512 ? 2 : 1) void page_few_kernel(const T *__restrict__ q, int64_t ldq,
                                                                                                        const T *__restrict__ cache, PaPlan pl, float qk, T *__restrict__ out,
@@ -545,7 +547,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, HD <= 128 && HD * (int)sizeof(T) * M
             if (mt && mt >= mts) continue;
             float x[8];
             pa_weights<T, DT>(pl, s[mt], qk, pos[mt], k0, held, whole, far, m[mt], l[mt], o[mt], seen[mt], x);
-            if constexpr (sizeof(T) == 2) pa_pack(x, false, ph[mt], plo[mt]);
+            if constexpr (sizeof(T) == 2) pa_pack(x, ph[mt], plo[mt]);
             else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x32[mt][e >> 2][e & 3] = x[e];
@@ -639,6 +641,9 @@ __global__ __launch_bounds__(64 * PA_WAVES, HD <= 128 && HD * (int)sizeof(T) * M
 // (no registers in between), each wave a quarter of each, while the step before is worked on; LDS holds two steps, so that one barrier a step is enough.
 // K units of positions 16 .. 31 change places by 8 there: the sixteen lanes of a read then cover all 64 banks.  Here the products bound, so weights are one
 // bf16 (8 bits, an error like that of the result's own rounding), and one more tile of values, all of them 1, gives their sums.
+// Prompts of 2040 and 1446 tokens, 32/8 heads of 128: 63 us, 815 TFLOP/s of what the mask leaves; matrix units are busy 39 % of the time (two waves a SIMD hold 253
+// registers each).  On the way (kernel under a tracer): records through registers 92 us (their copies to LDS, and spills whose reloads wait for the prefetches); a branch for each block's
+// reference 80; without 74; 67 with this part first (see below).
 template <int HD>
 __global__ __launch_bounds__(64 * PA_WAVES, 2) void page_many_kernel(const bf16_t *__restrict__ q, int64_t ldq, const bf16_t *__restrict__ cache, PaPlan pl, float qk,
                                                                      bf16_t *__restrict__ out, int64_t ldo, int vec, float *__restrict__ part)
@@ -831,13 +836,14 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void page_many_kernel(const bf16_
         const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
-            uint4 ph[MT], lo;
+            uint4 ph[MT];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 float x[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = pa_exp2(fmaf(s[mt][2 * i + (e >> 2)][e & 3], mul, -ref[mt]));
-                pa_pack(x, true, ph[mt], lo);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) (&ph[mt].x)[w] = bf16_pair(x[2 * w], x[2 * w + 1]);
             }
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
@@ -888,7 +894,8 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void page_many_kernel(const bf16_
 }
 
 // Joins the parts of rows that have several: those of their sequence's tile, then those of the prefix.  A workgroup takes 32 units (four values of a
-// row) of an own tile at a time, PA_JOIN threads each: a thread takes every PA_JOIN-th part, then they meet in LDS in order.
+// row) of an own tile at a time, PA_JOIN threads each: a thread takes every PA_JOIN-th part, then they meet in LDS in order.  4 us: a launch and three trips to memory in a row
+// (8 to 11 where it worked the cut out again instead of reading the words).
 #define PA_JOIN 8
 #define PA_UNITS 32
 template <typename T>
@@ -950,13 +957,18 @@ static int pa_plan(const sjd_pages *p, int rows, int n_seqs, int n_groups, int n
     pl->group_shift = pl->group & (pl->group - 1) ? -1 : __builtin_ctz((unsigned)pl->group);
     const int64_t entries = (int64_t)rows * pl->group;
     if (entries > INT32_MAX / 2) return SJD_EINVAL;
-    // Rows of a tile: what the segments have on average (a prefix is where most of a group's time goes).
+    // Rows of a tile.  More rows read a record less often, fewer leave more workgroups; only token counts are known here, not lengths.  us in a graph, 16 / 32 / 128 rows:
+    // 256 tokens of 32 heads 9.8 / 10.8 / 17.0; 512 tokens of 32/8 heads 17.8 / 16.1 / 20.7; 2 x 1000 tokens of 24 heads of 64
+    // 37.7 / 32.5 / 30.8; prompts of 2040 and 1446, 32/8 heads 163 / 136 / 67.  A prefix is read by all rows of its group: 16 queries of 32/8 heads behind 14 k
+    // positions 28 / 23 (16 / 32).
     const int64_t mean = (entries + n_seqs - 1) / n_seqs, most = n_groups ? std::max(mean, entries / n_groups) : mean;
     const int row = p->head_dim * (p->dtype ? 2 : 4);
     const bool many = p->dtype == 1 && p->head_dim <= 128 && most >= 64 && (entries >> 7) * p->n_kv_heads >= 256;
     const bool two = row <= 512 && ((n_groups && most > 16) || (entries >> 5) * p->n_kv_heads >= 384);
     pl->rows_shift = many ? 7 : two ? 5 : 4;
-    // Every segment has a last tile that is not full.
+    // Splits where tiles are few, as many as workgroups are resident, which registers decide (one query of 32 heads, 4 k positions, fp32: 32.7 with 512 splits, 35.4 with 384; 16
+    // queries behind a prefix, tiles of 32 rows, bf16: 27.0 with 384, 31.5 with 512).  Windows of many rows lose by being cut: 8 x 16 queries of 32 heads, 1.2 k positions, fp32
+    // 52 whole, 62 .. 68 cut.  Every segment has a last tile that is not full.
     const int64_t own = (entries >> pl->rows_shift) + n_seqs, shared = n_groups ? (entries >> pl->rows_shift) + n_groups : 0;
     const int64_t nblk = ((int64_t)width * p->page + 31) / 32;
     const bool few = own * p->n_kv_heads < (mean > 64 ? 320 : 512);
