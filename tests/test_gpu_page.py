@@ -313,6 +313,49 @@ def test_groups_and_starts_of_no_sense_stay_inside(B):
     assert (pad[:8] == 7).all() and (pad[16:] == 7).all()
 
 
+def test_starts_of_no_sense_in_tiles_of_many_rows(B):
+    c = Paged(B, 4, 8, 64, 32, 40, "bf16")
+    rows = 640
+    q, pad = rnd(3, rows, 64 * 64).to(torch.bfloat16).cuda(), torch.full((rows + 32, 64 * 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    for start, groups, prefix, length in (([0, 640, 4, 640, 640], [0, 4], [600], [100, 20, 30, 5]), ([-5, 300, 2 ** 31 - 1, 0, 640], [2, 1], [-7], [5, 5, 5, 5]),
+                                          ([0, 160, 320, 480, 640], [-2 ** 31, 2 ** 31 - 1], [2 ** 31 - 1], [2 ** 31 - 1, -2 ** 31, 1279, 1000])):
+        ws = torch.full((B.sjd_page_attention_workspace(c.pages, rows, 4, 1, 64, 40),), 0xFF, dtype=torch.uint8, device="cuda")
+        B.sjd_page_attention(c.pages, q, ints(start), ints(length), c.dev(), c.cache, pad[16:-16], ws, 0.125, groups=ints(groups), prefix=ints(prefix))
+    assert (pad[:16] == 7).all() and (pad[-16:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("pad", [1, 4, 8])
+def test_rows_of_wider_matrices(B, pad, dtype):
+    c = Paged(B, 2, 2, 96, 64, 20, dtype)
+    c.check([1100, 3], [2, 5], 6, pad=pad)
+    c.append([1100, 3], [2, 5], heads=3, t=B.sjd_rope_turns(10000.0, 32), pad=pad)
+
+
+def test_a_workspace_may_hold_anything(B):
+    """one workspace for calls of all kinds, one after the other, gives what a fresh one gives"""
+    c = Paged(B, 6, 2, 64, 32, 40, "bf16")
+    c.table[:, :8] = c.table[0, :8]
+    c.ref = host(c.cache)
+    calls = [([1000, 900, 800, 700, 600, 500], [9, 1, 2, 16, 3, 5], 8, dict(groups=[0, 6], prefix=[256])), ([300] * 6, [1] * 6, 4, {}), ([-1] * 6, [1] * 6, 4, {}),
+             ([1200, -1, 5, 7, 300, 256], [1, 1, 0, 0, 3, 1], 2, dict(groups=[3, 6], prefix=[256])), ([1100] * 6, [1] * 6, 8, dict(window=300, sinks=3)), ([1000] * 6, [30] * 6, 2, {})]
+    size = max(B.sjd_page_attention_workspace(c.pages, sum(t), 6, 1 if "groups" in kw else 0, h, 40) for _, t, h, kw in calls)
+    shared = torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda")
+    for rnd_ in range(2):
+        for n, t, h, kw in calls:
+            rows = sum(t)
+            start = ints(np.concatenate(([0], np.cumsum(t))).tolist())
+            q = rnd(7, rows, h * 64).to(torch.bfloat16).cuda()
+            more = {k: ints(v) if isinstance(v, list) else v for k, v in kw.items()}
+            outs = []
+            for ws in (shared, torch.zeros(size, dtype=torch.uint8, device="cuda")):
+                out = torch.full_like(q, 7.0)
+                B.sjd_page_attention(c.pages, q, start, ints(n), c.dev(), c.cache, out, ws, 0.125, **more)
+                outs.append(out)
+            assert torch.equal(*outs)
+            assert (outs[0][:1] == 7).all() == (n[0] < 0)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_what_masks_hide_does_not_matter(B, dtype):
     """NaN and infinities in masked positions, of the pages' unwritten rest and of later tokens"""
