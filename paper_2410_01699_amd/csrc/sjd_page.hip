@@ -177,20 +177,36 @@ __global__ __launch_bounds__(256) void page_append_kernel(PageSeqs sq, const T *
                 }
             }
         } else {
-            for (int w = lo * (HD / 2) + tid; w < hi * (HD / 2); w += 256) {
-                const int p = w / (HD / 2), i = w % (HD / 2);
-                int ea = 2 * i, eb = 2 * i + 1;
-                float c = 1.f, sn = 0.f;
-                const bool turns = i < ro.rot >> 1;
-                if (turns) { pair_at(ro, i, ea, eb); rope_angle(p0 + p, ro.turns[i], ro.magnitude, c, sn); }
+            // (four pairs' values are requested before the first is used)
+            for (int w0 = lo * (HD / 2) + tid; w0 < hi * (HD / 2); w0 += 4 * 256) {
+                T a[4][NH], b[4][NH];
+                int ea[4], eb[4];
 #pragma unroll
-                for (int j = 0; j < NH; ++j) {
-                    if (h0 + j >= heads) break;
-                    const T *src = q + (row0 + p) * ldq + (h0 + j) * HD;
-                    T *dst = q_out + (row0 + p) * ldqo + (h0 + j) * HD;
-                    const T a = src[ea], b = src[eb];
-                    dst[ea] = turns ? one_set<T>(fmaf(one_get(a), c, -one_get(b) * sn)) : a;
-                    dst[eb] = turns ? one_set<T>(fmaf(one_get(b), c, one_get(a) * sn)) : b;
+                for (int z = 0; z < 4; ++z) {
+                    const int w = min(w0 + z * 256, hi * (HD / 2) - 1), p = w / (HD / 2), i = w % (HD / 2);
+                    ea[z] = 2 * i; eb[z] = 2 * i + 1;
+                    if (i < ro.rot >> 1) pair_at(ro, i, ea[z], eb[z]);
+#pragma unroll
+                    for (int j = 0; j < NH; ++j) {
+                        const T *src = q + (row0 + p) * ldq + min(h0 + j, heads - 1) * HD;
+                        a[z][j] = src[ea[z]]; b[z][j] = src[eb[z]];
+                    }
+                }
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                    const int w = w0 + z * 256, p = w / (HD / 2), i = w % (HD / 2);
+                    if (w >= hi * (HD / 2)) break;
+                    const bool turns = i < ro.rot >> 1;
+                    float c = 1.f, sn = 0.f;
+                    if (turns) rope_angle(p0 + p, ro.turns[i], ro.magnitude, c, sn);
+#pragma unroll
+                    for (int j = 0; j < NH; ++j) {
+                        if (h0 + j >= heads) break;
+                        T *dst = q_out + (row0 + p) * ldqo + (h0 + j) * HD;
+                        const T x = a[z][j], y = b[z][j];
+                        dst[ea[z]] = turns ? one_set<T>(fmaf(one_get(x), c, -one_get(y) * sn)) : x;
+                        dst[eb[z]] = turns ? one_set<T>(fmaf(one_get(y), c, one_get(x) * sn)) : y;
+                    }
                 }
             }
         }
@@ -215,6 +231,7 @@ __global__ __launch_bounds__(256) void page_append_kernel(PageSeqs sq, const T *
             eight_store(&tile[1][p * PITCH + 16 * u], c); eight_store(&tile[1][p * PITCH + 16 * u + 8], d);
         }
     } else {
+#pragma unroll 4
         for (int w = lo * (HD / 2) + tid; w < hi * (HD / 2); w += 256) {
             const int p = w / (HD / 2), i = w % (HD / 2);
             const T *ks = k + (row0 + p) * ld + y * HD, *vs = v + (row0 + p) * ld + y * HD;
