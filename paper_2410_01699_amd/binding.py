@@ -632,8 +632,6 @@ def sjd_page_append(pages, k, v, start, length, table, cache, turns=None, interl
     pv, dv, lv = _rows(dev, "v", v, rows, cols)
     if dt != pages.dtype or dv != dt:
         _refuse("k, v and the pool have one type")
-    if rows == 1:
-        lv = ld
     if lv != ld:
         _refuse("k and v have the same stride")
     pq = pqo = None
@@ -655,12 +653,12 @@ def sjd_page_append(pages, k, v, start, length, table, cache, turns=None, interl
 @functools.lru_cache(maxsize=4096)
 def _page_workspace(shape, rows, n_seqs, n_groups, n_heads, width) -> int:
     n = _sz(0)
-    _check(_lib.sjd_page_attention_workspace(C.byref(sjd_pages(*shape)), rows, n_seqs, n_groups, n_heads, width, C.byref(n)))
+    _check(_lib.sjd_page_attention_workspace(C.byref(sjd_pages.from_buffer_copy(shape)), rows, n_seqs, n_groups, n_heads, width, C.byref(n)))
     return n.value
 
 
 def sjd_page_attention_workspace(pages, rows, n_seqs, n_groups, n_heads, width) -> int:
-    return _page_workspace((pages.dtype, pages.n_kv_heads, pages.head_dim, pages.page, pages.n_pages), rows, n_seqs, n_groups, n_heads, width)
+    return _page_workspace(bytes(pages), rows, n_seqs, n_groups, n_heads, width)
 
 
 def sjd_page_attention(pages, q, start, length, table, cache, out, workspace, scale, window=0, sinks=0, groups=None, prefix=None, stream=None):
