@@ -114,8 +114,10 @@ __device__ __forceinline__ int pa_tiles(const PaPlan &pl, const PaSeg &sg) { ret
 
 // What a slot is: its segment, tile and split, the first slot of the segment, and of own segments the number of its first tile among the own ones
 struct PaPart { PaSeg sg; int32_t seg, tile, split, splits, per, base, own; };
-// Lanes look at 64 segments at a time, c0: those of the first 64.  by_seg: the first slot of the given segment.  own_total: all own tiles, if it is found in
-// the walk's last 64.  With per >= total / slots the splits of all tiles are at most slots + tiles.
+// Lanes look at 64 segments at a time, c0: those of the first 64.  by_seg: the first slot of the given segment.  own_total: the own tiles whose first slot is launched, if
+// the walk gets to its last 64.  With per >= total / slots the splits of all tiles are at most slots + tiles, so that these are all; starts or groups without sense can ask for
+// more slots than there are, and the tiles behind them have no word (the join would take what an earlier call left for one) and do not count.  Counts stay below 2^31 there too: no segment's
+// above 2^24, no sum before 64 of them above 2^29, both more than a launch has.
 __device__ __forceinline__ bool pa_part(const PaPlan &pl, const PaSeg &c0, int per, int want, bool by_seg, PaPart &part, int &own_total)
 {
     const int n = pl.n_groups + pl.sq.n_seqs, lane = threadIdx.x & 63;
@@ -124,8 +126,11 @@ __device__ __forceinline__ bool pa_part(const PaPlan &pl, const PaSeg &c0, int p
         const PaSeg sg = s0 == 0 ? c0 : s0 + lane < n ? pa_segment(pl, s0 + lane) : PaSeg{};
         const bool prefix = s0 + lane < pl.n_groups;
         const int splits = max((int)(((int64_t)sg.count + per - 1) / per), !prefix && sg.m ? 1 : 0);     // (of own segments one at least, which may be empty)
-        const int tiles = splits ? pa_tiles(pl, sg) : 0, mine = tiles * splits, mine_own = prefix ? 0 : tiles;
-        const int incl = page_sum_up(mine), incl_own = page_sum_up(mine_own), begin = base + incl - mine;
+        const int tiles = splits ? pa_tiles(pl, sg) : 0, mine = (int)min((int64_t)tiles * splits, (int64_t)1 << 24);
+        const int incl = page_sum_up(mine), begin = base + incl - mine;
+        int mine_own = prefix ? 0 : tiles;
+        if (mine_own && begin + mine > pl.items) mine_own = max(0, pl.items - begin + splits - 1) / splits;
+        const int incl_own = page_sum_up(mine_own);
         const uint64_t hit = by_seg ? __ballot(s0 + lane == want) : __ballot(want >= begin && want < begin + mine);
         own_total = own + page_lane(incl_own, 63);
         if (hit) {
@@ -141,7 +146,7 @@ __device__ __forceinline__ bool pa_part(const PaPlan &pl, const PaSeg &c0, int p
             part.split = at - part.tile * d;
             return true;
         }
-        base += page_lane(incl, 63);
+        base = min(base + page_lane(incl, 63), 1 << 29);
         own = own_total;
     }
     return false;
@@ -160,7 +165,7 @@ __device__ __forceinline__ int pa_per(const PaPlan &pl, const PaSeg &c0)
 }
 
 // Word of an own tile for the kernel that joins its parts: its first row and entries, its tile, its first slot and splits, those of the prefix's first tile, and what its
-// entries' numbers are higher there.  In front of all: the number of own tiles.
+// entries' numbers are higher there.  In front of all: the number of words.
 struct PaWord { int32_t r0, entries, tile, base1, splits1, base2, splits2, above; };
 __device__ __forceinline__ PaWord *pa_words(float *part) { return reinterpret_cast<PaWord *>(part) + 1; }
 
