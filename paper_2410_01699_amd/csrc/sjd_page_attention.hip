@@ -10,6 +10,7 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 #define PA_WAVES 4
 #define PA_TOP 16.f                       // a row's reference stays until a score is 2^PA_TOP above it
 #define PA_NONE -3.4028234664e38f         // reference of a row that has seen nothing: finite, so that differences need no cases
+#define PA_LOW -3.4028e38f               // least reference of a row that has seen something: what overflows downwards weighs nothing against it
 #define PA_FAR 1048576.f                  // references from here on: fp32 has 1/8 between scores
 
 // The work is cut three ways.  A segment is what queries and keys have in common: the queries of one sequence over its own positions, or those of
@@ -327,7 +328,7 @@ __device__ __forceinline__ void pa_weights(const PaPlan &pl, const f32x4 (&s)[2]
         bm = fmaxf(fmaxf(s[0][0], s[0][1]), s[0][2]);
         bm = fmaxf(fmaxf(bm, s[0][3]), s[1][0]);
         bm = fmaxf(fmaxf(bm, s[1][1]), s[1][2]);
-        bm = fmaxf(bm, s[1][3]) * qk;
+        bm = fmaxf(fmaxf(bm, s[1][3]) * qk, PA_LOW);
     } else {
         seen = 0;
         bm = -INFINITY;
@@ -338,6 +339,7 @@ __device__ __forceinline__ void pa_weights(const PaPlan &pl, const f32x4 (&s)[2]
             seen |= see ? 1u << e : 0u;
             bm = fmaxf(bm, see ? s[e >> 2][e & 3] * qk : -INFINITY);
         }
+        bm = fmaxf(bm, seen ? PA_LOW : -INFINITY);
     }
     if (__ballot(bm - m > PA_TOP)) {
         const float mn = fmaxf(m, pa_across(bm)), turn = pa_exp2(m - mn);
@@ -345,7 +347,7 @@ __device__ __forceinline__ void pa_weights(const PaPlan &pl, const f32x4 (&s)[2]
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[t] *= turn;
         m = mn;
-        far |= __ballot(fabsf(mn) >= PA_FAR && mn > PA_NONE) != 0;
+        far |= __ballot(fabsf(mn) >= PA_FAR && mn > PA_LOW) != 0;
     }
     if (whole && !far) {
 #pragma unroll
@@ -397,6 +399,8 @@ __device__ __forceinline__ uint32_t pa_marks(uint4 &v, float)
     }
     return marks;
 }
+// What a row's sums are multiplied by: nothing where it has seen nothing, NaN where it has seen only scores that overflowed downwards
+__device__ __forceinline__ float pa_norm(float m, float l) { return l != 0.f ? 1.f / l : m > PA_NONE ? NAN : 0.f; }
 // NaN to the sums o (of a tile of dimensions whose units' marks are given) of the rows that see a marked value
 template <typename T, int VU>
 __device__ __forceinline__ void pa_taint(const uint32_t (&marks)[VU], uint32_t seen, f32x4 &o)
@@ -620,7 +624,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, HD <= 128 && HD * (int)sizeof(T) * M
         for (int w = 0; w < PA_WAVES; ++w) M = fmaxf(M, m_all[w][mt][c]);
 #pragma unroll
         for (int w = 0; w < PA_WAVES; ++w) den += pa_exp2(m_all[w][mt][c] - M) * l_all[w][mt][c];
-        const float turn = pa_exp2(m[mt] - M), norm = den == 0.f ? 0.f : 1.f / den;
+        const float turn = pa_exp2(m[mt] - M), norm = pa_norm(M, den);
         const int entry = e0 + 16 * mt + c, i = pa_div(pl, min(entry, entries - 1));
 #pragma unroll
         for (int t0 = 0; t0 < DT; t0 += CH) {
@@ -772,6 +776,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void page_many_kernel(const bf16_
         for (int t = 0; t < DT; ++t) va[t] = *reinterpret_cast<const uint4 *>(buf + vat + P::v_at(t, 0));
         const int last = k0[NB - 1] + 31;
         const bool whole = held == 3u && __ballot(!(last <= low)) == 0 && (pl.window == 0 || last < pl.sinks || (wk.own && k0[0] > high - pl.window));
+        float least[MT] = {PA_LOW, PA_LOW};
         if (edge) {
             uint32_t seen[MT];
 #pragma unroll
@@ -786,6 +791,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void page_many_kernel(const bf16_
                     seen[mt] |= see ? 1u << e : 0u;
                     s[mt][e >> 2][e & 3] = see ? s[mt][e >> 2][e & 3] : -INFINITY;
                 }
+                least[mt] = seen[mt] ? PA_LOW : -INFINITY;
             }
             // (also where this wave's rows see all: the values were taken out for the others)
             if (wild[n & 1][0] | wild[n & 1][1] | wild[n & 1][2] | wild[n & 1][3]) {
@@ -808,7 +814,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void page_many_kernel(const bf16_
             bm[mt] = s[mt][0][0];
 #pragma unroll
             for (int e = 1; e + 1 < 8 * NB; e += 2) bm[mt] = fmaxf(fmaxf(bm[mt], s[mt][e >> 2][e & 3]), s[mt][(e + 1) >> 2][(e + 1) & 3]);
-            bm[mt] = fmaxf(bm[mt], s[mt][2 * NB - 1][3]) * qk;
+            bm[mt] = fmaxf(fmaxf(bm[mt], s[mt][2 * NB - 1][3]) * qk, least[mt]);
         }
         if (__ballot((bm[0] - m[0] > PA_TOP) | (bm[1] - m[1] > PA_TOP))) {
 #pragma unroll
@@ -817,7 +823,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void page_many_kernel(const bf16_
 #pragma unroll
                 for (int t = 0; t <= DT; ++t) o[mt][t] *= turn;
                 m[mt] = mn;
-                far |= __ballot(fabsf(mn) >= PA_FAR && mn > PA_NONE) != 0;
+                far |= __ballot(fabsf(mn) >= PA_FAR && mn > PA_LOW) != 0;
             }
         }
 #pragma unroll
@@ -883,7 +889,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, 2) void page_many_kernel(const bf16_
     float *dst = part + 8 + 8 * (size_t)pl.tiles + ((size_t)head * pl.items + slot) * pa_record(ROWS, HD);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-        const float l = o[mt][DT][0], norm = l == 0.f ? 0.f : 1.f / l;
+        const float l = o[mt][DT][0], norm = pa_norm(m[mt], l);
         const int r = wave * RW + 16 * mt + c, entry = wk.e0 + r;
         if (entry >= wk.entries) continue;
         if (wk.alone) {
@@ -947,7 +953,7 @@ __global__ __launch_bounds__(PA_UNITS * PA_JOIN) void page_merge_kernel(const fl
 #pragma unroll
             for (int j = 1; j < PA_JOIN; ++j) add(red[j][0][x], red[j][1][x], acc[j][x]);
             const int i = pa_div(pl, entry), h = entry - i * pl.group;
-            pa_out(out + (int64_t)(w.r0 + i) * ldo + ((int64_t)head * pl.group + h) * hd + d, a * (den == 0.f ? 0.f : 1.f / den), vec & 2);
+            pa_out(out + (int64_t)(w.r0 + i) * ldo + ((int64_t)head * pl.group + h) * hd + d, a * pa_norm(M, den), vec & 2);
         }
         __syncthreads();
     }
