@@ -473,7 +473,8 @@ int sjd_page_append(const sjd_pages *pages, const void *q, int64_t ldq, int32_t 
  * none.  With window > 0 groups are not used.
  * scale is finite and above zero.  Scores and sums are fp32, bf16 probabilities have at least 8 bits.  A visible score that overflows upwards gives NaN; those that overflow
  * downwards weigh nothing, and a query that sees no others gives NaN.  A visible infinity or NaN among the values
- * gives an infinity or NaN in that dimension.  What masked positions hold, NaN included, does not reach `out`.  workspace: sjd_page_attention_workspace bytes (may be 0), 16-byte aligned.
+ * gives an infinity or NaN in that dimension, and so may a finite one above 2^80: sums are up to 2^16 times what the softmax weighs, times the positions.
+ * What masked positions hold, NaN included, does not reach `out`.  workspace: sjd_page_attention_workspace bytes (may be 0), 16-byte aligned.
  * rows <= 2^24, n_seqs <= 65535, heads <= 4096.                                                  */
 int sjd_page_attention_workspace(const sjd_pages *pages, int32_t rows, int32_t n_seqs, int32_t n_groups, int32_t n_heads, int32_t width, size_t *bytes);
 int sjd_page_attention(const sjd_pages *pages, const void *q, int64_t ldq, int32_t n_heads, int32_t rows, const int32_t *start, const int32_t *len, int32_t n_seqs,

@@ -35,7 +35,7 @@ def test_the_join_takes_no_word_of_another_call(B, n_seqs, tokens, heads, kv, wi
 # ---- scores at the ends of their range ----------------------------------------------------------------
 # (length, tokens, heads, kv heads, width in pages of 32, more): one walk; cut walks; a shared prefix; 128-row tiles in bf16, with edges, cut, and behind a prefix
 SHAPES = [([7, 40], [70, 3], 4, 2, 8, {}), ([1200, 3], [2, 1], 4, 2, 42, {}), ([100, 70, 64], [1, 9, 2], 8, 2, 8, dict(groups=[0, 3], prefix=[64])),
-          ([900, 950], [1, 2], 8, 2, 40, dict(groups=[0, 2], prefix=[896])), ([0, 300], [320, 129], 64, 8, 26, {}), ([1100], [130], 64, 4, 40, {}),
+          ([900, 950], [1, 2], 8, 2, 40, dict(groups=[0, 2], prefix=[896])), ([0, 300], [320, 129], 64, 8, 26, {}), ([1100], [520], 64, 8, 52, {}),
           ([128, 140], [200, 130], 64, 8, 26, dict(groups=[0, 2], prefix=[128]))]
 
 
@@ -85,7 +85,7 @@ def test_scores_that_overflow(B, length, tokens, heads, kv, width, more, hd, dty
             k, v, _ = R.sequence(c.ref, c.table[b], 32, n + tokens[b], c.bf16)
             for p in range(n, n + tokens[b]):
                 some = [j for j in range(low, p + 1)]
-                for h in range(heads):
+                for h in range(row % 5, heads, 1 if len(got) < 100 else 13):
                     if not some or some[-1] >= last and last >= low:
                         assert np.isnan(got[row, h]).all(), (low, b, p)
                         continue
@@ -97,6 +97,58 @@ def test_scores_that_overflow(B, length, tokens, heads, kv, width, more, hd, dty
                     room = (np.expm1(2 * d) + 2.0 ** -20 + (len(some) / 4 + 64) * 2.0 ** -24 + (2.0 ** -8 if c.bf16 else 0)) * top
                     assert (np.abs(got[row, h] - want) <= room + own(np.abs(want) + room, dtype)).all(), (low, b, p, h)
                 row += 1
+
+
+LN2 = float(np.float32(np.log(2)))              # (times log2 e, in fp32, is 1: a score is then a power of two as the product gives it)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("length,tokens,heads,kv,width,more", SHAPES)
+def test_scores_far_off_with_small_differences(B, length, tokens, heads, kv, width, more, hd, dtype):
+    """Whole-number scores 2^22 below zero, about it or 2^22 above it, by rows, and for half of the heads 2^21 more from the middle on: all exact in fp32, so weights are as well as near zero"""
+    rng = np.random.RandomState(1)
+    mid = (length[0] + tokens[0]) // 2
+
+    def keys(p, k):
+        k = np.zeros_like(k)
+        k[:, 0], k[:, 1] = 2.0 ** 11, 2.0 ** 10 if p >= mid else 0.0
+        k[:, 2:10] = rng.randint(-2, 3, (len(k), 8))
+        return k
+    c = filled(B, length, tokens, kv, width, more, hd, dtype, keys)
+    q = np.zeros((sum(tokens), heads, hd))
+    q[..., 0] = np.array([-1.0, 0.0, 1.0, 1.0, -1.0])[np.arange(len(q)) * 7 // 3 % 5, None] * 2.0 ** 11
+    q[:, ::2, 1] = 2.0 ** 11
+    q[..., 2:10] = rng.randint(-1, 2, (len(q), heads, 8))
+    got, q = attended(c, q, length, tokens, heads, LN2, more)
+    start = np.concatenate(([0], np.cumsum(tokens)))
+    want, _, top = R.attention(c.ref, q, start, length, c.table, 32, LN2, c.bf16)
+    n = max(x + y for x, y in zip(length, tokens))
+    # (differences up to 64 times ln 2's own rounding, below 2^-21)
+    room = (2.0 ** -20 + 2.0 ** -21 + (n / 4 + 64) * 2.0 ** -24 + (2.0 ** -8 if c.bf16 else 0)) * top[..., None]
+    assert (np.abs(got - want) <= room + own(np.abs(want) + room, dtype)).all(), np.max(np.abs(got - want) / room)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("length,tokens,heads,kv,width,more", SHAPES)
+def test_large_values_behind_a_late_reference(B, length, tokens, heads, kv, width, more, dtype):
+    """Values up to 2^80 stay finite where later scores are as far above the first ones as a reference may lag, 2^15 in weight"""
+    def keys(p, k):
+        k = np.zeros_like(k)
+        k[:, 0] = 15.0 if p % 64 >= 32 or p > 600 else 0.0
+        return k
+    c = filled(B, length, tokens, kv, width, more, 64, dtype, keys)
+    at = R.record_at(64, c.bf16)[1].reshape(-1)
+    c.ref[..., at] *= 2.0 ** 78 / np.abs(c.ref[..., at]).max()
+    c.cache.copy_(torch.from_numpy(c.ref))
+    c.ref = host(c.cache)
+    q = np.zeros((sum(tokens), heads, 64))
+    q[..., 0] = 1.0
+    got, q = attended(c, q, length, tokens, heads, LN2, more)
+    want, _, top = R.attention(c.ref, q, np.concatenate(([0], np.cumsum(tokens))), length, c.table, 32, LN2, c.bf16)
+    n = max(x + y for x, y in zip(length, tokens))
+    room = (2.0 ** -20 + 2.0 ** -21 + (n / 4 + 64) * 2.0 ** -24 + (2.0 ** -8 if c.bf16 else 0)) * top[..., None]
+    assert (np.abs(got - want) <= room + own(np.abs(want) + room, dtype)).all(), np.max(np.abs(got - want) / room)
 
 
 def test_rows_that_see_nothing_give_zeros(B):
