@@ -5,6 +5,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 import page_reference as R  # noqa: E402
+import test_gpu_page as G  # noqa: E402
 from test_gpu_page import B, Paged, host, ints, own, rnd  # noqa: E402, F401
 
 pytestmark = pytest.mark.gpu
@@ -160,3 +161,85 @@ def test_rows_that_see_nothing_give_zeros(B):
             c.cache[0] = float("nan")
             got, _ = attended(c, rnd(4, sum(tokens), heads, 64).double().numpy(), length, tokens, heads, 0.125, more)
             assert (got == 0).all()
+
+
+# ---- every kernel and every variant -------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rows,heads,hd,rot,pad", [(1201, 33, 128, 128, 16), (2001, 41, 64, 32, 0), (1501, 31, 96, 96, 8), (601, 30, 256, 64, 0), (4100, 65, 16, 16, 0)])
+def test_many_rows_are_turned(B, rows, heads, hd, rot, pad, interleaved, dtype):
+    """four heads a thread, heads that are no multiple of four: near the definition, and to the bit what a call for each 32 rows (one head a thread) gives"""
+    assert rows * heads * (hd // 16) >= 1 << 18 > 32 * heads * (hd // 16)
+    G.test_rows_are_turned(B, rows, heads, hd, rot, pad, interleaved, dtype)
+    t, turns = G.table_of(B, rot)
+    x = rnd(1, rows, heads * hd).to(G.TYPES[dtype]).cuda()
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda") * 911 - 70000
+    whole, parts = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    B.sjd_rope(x, whole, pos, hd, turns, interleaved=interleaved, magnitude=1.5)
+    for r in range(0, rows, 32):
+        B.sjd_rope(x[r:r + 32], parts[r:r + 32], pos[r:r + 32], hd, turns, interleaved=interleaved, magnitude=1.5)
+    assert torch.equal(whole, parts)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n_seqs,tokens,kv,hd,page,heads,rot,interleaved,pad", [
+    (3, 230, 1, 64, 32, 77, 64, False, 0), (3, 230, 1, 64, 64, 77, 32, True, 16), (3, 230, 1, 64, 32, 76, 10, False, 0), (2, 300, 2, 32, 32, 161, 32, False, 3), (40, 3, 1, 128, 32, 25, 128, True, 0),
+    (40, 3, 3, 96, 32, 25, 94, True, 0), (40, 2, 1, 256, 32, 27, 256, False, 0), (40, 2, 1, 256, 64, 27, 254, False, 0), (2, 500, 8, 128, 64, 107, 64, False, 0)])
+def test_append_with_many_heads(B, n_seqs, tokens, kv, hd, page, heads, rot, interleaved, pad, dtype):
+    """two query heads a workgroup, odd numbers of them, by units and by values; ragged tokens"""
+    lengths = [(b * 37) % 50 for b in range(n_seqs)]
+    counts = [max(0, tokens - b % 3) for b in range(n_seqs)]
+    assert (sum(counts) // 32 + 2 * n_seqs) * heads >= 2048
+    c = Paged(B, n_seqs, kv, hd, page, -(-(tokens + 60) // page), dtype)
+    t = B.sjd_rope_turns(10000.0, rot)
+    c.append(lengths, counts, seed=1, heads=heads, t=t, interleaved=interleaved, pad=pad, behind=2)
+    lengths[1] = -1                                 # sits out
+    c.append(lengths, counts, seed=2, heads=heads, t=t, interleaved=interleaved, magnitude=1.2, pad=pad, inplace=True)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("hd", [32, 64, 96, 128, 256])
+@pytest.mark.parametrize("length,tokens,heads,kv,kw", [
+    ([0, 700], [300, 100], 32, 8, {}), ([0, 700], [300, 100], 32, 8, dict(window=90, sinks=40)), ([20, 31], [150, 263], 32, 8, dict(pad=1)), ([160, 130, 128], [1, 9, 2], 8, 2, dict(groups=[0, 3], prefix=[128])),
+    ([800, 810, -1, 790], [3, 9, 2, 20], 16, 2, dict(groups=[0, 4], prefix=[770]))])
+def test_tiles_of_32_rows(B, length, tokens, heads, kv, kw, hd, dtype):
+    c = Paged(B, len(length), kv, hd, 32, 27, dtype)
+    if "prefix" in kw:
+        c.table[:, :kw["prefix"][0] // 32] = c.table[0, :kw["prefix"][0] // 32]
+    assert "prefix" in kw or (sum(tokens) * heads // kv >> 5) * kv >= 384
+    c.check(length, tokens, heads, **kw)
+
+
+@pytest.mark.parametrize("hd", [32, 64, 96, 128])
+@pytest.mark.parametrize("length,tokens,kw", [([1100], [520], {}), ([900, 40], [290, 240], {}), ([1000, 1000], [260, 260], dict(groups=[0, 2], prefix=[992])), ([1100], [520], dict(window=200, sinks=50)),
+                                              ([1030, 1100, 1024], [100, 257, 170], dict(groups=[1, 3], prefix=[512]))])
+def test_tiles_of_many_rows_over_cut_walks(B, length, tokens, kw, hd):
+    c = Paged(B, len(length), 8, hd, 32, 52, "bf16")
+    if "prefix" in kw:
+        first, last = kw["groups"]
+        c.table[first:last, :kw["prefix"][0] // 32] = c.table[first, :kw["prefix"][0] // 32]
+    own_tiles = (sum(tokens) * 8 >> 7) + len(length)
+    assert (sum(tokens) * 8 >> 7) * 8 >= 256 and own_tiles * 8 < 320
+    assert B.sjd_page_attention_workspace(c.pages, sum(tokens), len(length), 0, 64, 52) > 0           # walks are cut
+    c.check(length, tokens, 64, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("hd", [32, 96, 128, 256])
+@pytest.mark.parametrize("length,tokens,heads,kv,window,sinks", [([1300], [1], 4, 4, 0, 0), ([1500, 3, 700, 1100], [1, 1, 2, 16], 4, 2, 0, 0), ([1500, 40, 1030], [5, 60, 1], 4, 2, 33, 40), ([1023, 1024, 1025], [1, 1, 1], 8, 1, 0, 0)])
+def test_cut_walks_of_all_heads(B, length, tokens, heads, kv, window, sinks, hd, dtype):
+    Paged(B, len(length), kv, hd, 64, 26, dtype).check(length, tokens, heads, window, sinks)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n_seqs,width", [(65, 5), (90, 34)])
+def test_tiles_of_many_rows_of_more_sequences_than_lanes(B, n_seqs, width, hd):
+    c = Paged(B, n_seqs, 8, hd, 32, width, "bf16")
+    groups, prefix = [2, 40, n_seqs - 1], [96, 64]
+    for g, p in enumerate(prefix):
+        c.table[groups[g]:groups[g + 1], :p // 32] = c.table[groups[g], :p // 32]
+    length, tokens = [96 + (b * 7) % 20 for b in range(n_seqs)], [20 - b % 4 for b in range(n_seqs)]
+    length[5] = -1
+    assert sum(tokens) * 8 // n_seqs >= 64 and (sum(tokens) * 8 >> 7) * 8 >= 256
+    c.check(length, tokens, 64, groups=groups, prefix=prefix)
+    c.check(length, tokens, 64, behind=3)
