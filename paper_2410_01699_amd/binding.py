@@ -625,7 +625,7 @@ def sjd_page_append(pages, k, v, start, length, table, cache, turns=None, interl
     table: int32 [n_seqs, width], all on the device"""
     dev = _device(k)
     rows, cols = _matrix("k", k)
-    if cols != pages.n_kv_heads * pages.head_dim:
+    if pages.head_dim < 1 or cols != pages.n_kv_heads * pages.head_dim:
         _refuse(f"k has {cols} columns, the pool {pages.n_kv_heads} heads of {pages.head_dim}")
     n_seqs, width, ps, pl, pt, pc = _paged(dev, pages, start, length, table, cache)
     pk, dt, ld = _rows(dev, "k", k, rows, cols)
@@ -665,7 +665,7 @@ def sjd_page_attention(pages, q, start, length, table, cache, out, workspace, sc
     """q, out: device [rows, n_heads * head_dim]; groups: int32 [n_groups + 1] and prefix: int32 [n_groups] on the device, or neither"""
     dev = _device(q)
     rows, cols = _matrix("q", q)
-    if cols % pages.head_dim:
+    if pages.head_dim < 1 or cols % pages.head_dim:
         _refuse("q has whole heads")
     n_seqs, width, ps, pl, pt, pc = _paged(dev, pages, start, length, table, cache)
     pq, dt, ldq = _rows(dev, "q", q, rows, cols)

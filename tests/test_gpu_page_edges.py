@@ -243,3 +243,14 @@ def test_tiles_of_many_rows_of_more_sequences_than_lanes(B, n_seqs, width, hd):
     assert sum(tokens) * 8 // n_seqs >= 64 and (sum(tokens) * 8 >> 7) * 8 >= 256
     c.check(length, tokens, 64, groups=groups, prefix=prefix)
     c.check(length, tokens, 64, behind=3)
+
+
+def test_a_pool_of_no_dimensions_is_refused(B):
+    x, i, cache = torch.zeros(2, 64, device="cuda"), ints([0, 2]), torch.zeros(0, device="cuda")
+    for hd in (0, -64):
+        p = B.sjd_pages(0, 1, hd, 32, 1)
+        for f in (lambda: B.sjd_page_attention(p, x, i, i[1:], i[:1].view(1, 1), cache, x, None, 1.0),
+                  lambda: B.sjd_page_append(p, x[:, :0], x[:, :0], i, i[1:], i[:1].view(1, 1), cache, q=x, q_out=x)):
+            with pytest.raises(B.SjdError) as e:
+                f()
+            assert e.value.code == B.SJD_EINVAL
