@@ -457,7 +457,7 @@ int sjd_rope(int32_t dtype, const void *x, int64_t ldx, void *out, int64_t ldo, 
  * page outside the pool nothing is stored, and nothing is seen.  len is the caller's to advance; tokens may be appended again at the same or a smaller len.  */
 typedef struct { int32_t dtype, n_kv_heads, head_dim, page, n_pages; } sjd_pages;
 
-/* k, v dev [rows x n_kv_heads * head_dim] (rows of length ld) into the pages, keys turned by their positions (turns NULL and rot_dim 0: as they are).  Other positions of the
+/* k, v dev [rows x n_kv_heads * head_dim] (rows of length ld) into the pages, keys turned by their positions (turns NULL and rot_dim 0: as they are, without queries).  Other positions of the
  * records keep what they hold; a page that is written belongs to one sequence of the call.  q dev [rows x n_heads * head_dim], turned likewise, goes to q_out (which may
  * be q); both NULL: keys and values only.                                                        */
 int sjd_page_append(const sjd_pages *pages, const void *q, int64_t ldq, int32_t n_heads, void *q_out, int64_t ldqo, const void *k, const void *v, int64_t ld,
@@ -466,12 +466,12 @@ int sjd_page_append(const sjd_pages *pages, const void *q, int64_t ldq, int32_t 
 
 /* Attention of the new tokens' queries q dev [rows x n_heads * head_dim] (as they are: turned already) over the pages, the tokens' own keys included:
  * softmax(scale q k) v -> out, like q, rows of length ldo.  The query at position p sees the positions j <= p with, if window > 0, also j > p - window or j < sinks; one
- * that sees nothing gives zeros.  Query head h reads cache head h / (n_heads / n_kv_heads).
+ * that sees nothing gives zeros.  (A prompt takes no less time for a window: all its tiles walk from the first block that its first token sees.)  Query head h reads cache head h / (n_heads / n_kv_heads).
  * Groups: the sequences groups[g] .. groups[g + 1] - 1 (groups dev int32 [n_groups + 1], ascending) begin with the same prefix[g] positions (dev int32 [n_groups]), say
  * images of one prompt, and their table rows name the same pages for the whole pages of it, prefix[g] / page of them: those are read and weighed once for all.
  * (What is left of the prefix lies in pages that each sequence goes on in, so in copies.)  The result does not depend on it but for the order of sums.  n_groups 0:
  * none.  With window > 0 groups are not used.
- * scale is finite and above zero.  Scores and sums are fp32, bf16 probabilities have at least 8 bits.  A visible score that overflows upwards gives NaN; those that overflow
+ * scale is above zero and below 1e30.  Scores and sums are fp32, bf16 probabilities have at least 8 bits.  A visible score that overflows upwards gives NaN; those that overflow
  * downwards weigh nothing, and a query that sees no others gives NaN.  A visible infinity or NaN among the values
  * gives an infinity or NaN in that dimension, and so may a finite one above 2^80: sums are up to 2^16 times what the softmax weighs, times the positions.
  * What masked positions hold, NaN included, does not reach `out`.  workspace: sjd_page_attention_workspace bytes (may be 0), 16-byte aligned.

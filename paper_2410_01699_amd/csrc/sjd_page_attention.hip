@@ -220,7 +220,6 @@ template <int HD, typename T> struct PaTile {
     static constexpr int KS = B16 ? HD / 32 : HD / 16;         // 16-byte units of a row to a lane
     static constexpr int DT = HD / 16;
     static constexpr int VU = B16 ? 1 : 2;                     // units of values to a tile of 16 dimensions
-    static constexpr int NK = 2 * KS, NV = DT * VU;            // loads a block
     // bytes into a record: what a lane adds, and what is the same for all
     __device__ static __forceinline__ int k_lane(int lane) { return 16 * ((lane >> 4) * 32 + PaOps<T>::position(0, lane & 15)); }
     static constexpr int k_at(int a, int ks) { return 16 * (128 * ks + (B16 ? 8 : 16) * a); }
@@ -257,7 +256,7 @@ template <> __device__ __forceinline__ void pa_out<bf16_t>(bf16_t *p, const f32x
 
 // What a workgroup is about.  own: a sequence's own positions; alone: the only part of its rows; [gs, ge): a group's sequences; entries e0 .. of the segment's, each a
 // row and a head; blocks [beg, end) of the segment's; first: (of a prefix) no row stands before this position.
-struct PaWork { PaSeg sg; int32_t seg, own, alone, gs, ge, e0, entries, beg, end, first; };
+struct PaWork { PaSeg sg; int32_t own, alone, gs, ge, e0, entries, beg, end, first; };
 __device__ __forceinline__ bool pa_work(const PaPlan &pl, int head, int slot, int32_t (*known)[3], float *part, PaWork &w)
 {
     const int lane = threadIdx.x & 63, rows = 1 << pl.rows_shift, n = pl.n_groups + pl.sq.n_seqs;
@@ -273,7 +272,7 @@ __device__ __forceinline__ bool pa_work(const PaPlan &pl, int head, int slot, in
         if (lane == 0) *reinterpret_cast<int32_t *>(part) = total;
     }
     if (!some) return false;
-    w.sg = pt.sg; w.seg = pt.seg;
+    w.sg = pt.sg;
     w.own = pt.seg >= pl.n_groups;
     w.alone = w.own && pt.splits == 1 && pt.sg.g < 0;
     if (w.own && writer && pt.split == 0) {
@@ -650,7 +649,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, HD <= 128 && HD * (int)sizeof(T) * M
 // (no registers in between), each wave a quarter of each, while the step before is worked on; LDS holds two steps, so that one barrier a step is enough.
 // K units of positions 16 .. 31 change places by 8 there: the sixteen lanes of a read then cover all 64 banks.  Here the products bound, so weights are one
 // bf16 (8 bits, an error like that of the result's own rounding), and one more tile of values, all of them 1, gives their sums.
-// Prompts of 2040 and 1446 tokens, 32/8 heads of 128: 63 us, 815 TFLOP/s of what the mask leaves; matrix units are busy 39 % of the time (two waves a SIMD hold 253
+// Prompts of 2040 and 1446 tokens, 32/8 heads of 128: 63.6 us, 805 TFLOP/s of what the mask leaves; matrix units are busy 39 % of the time (two waves a SIMD hold 255
 // registers each).  On the way (kernel under a tracer): records through registers 92 us (their copies to LDS, and spills whose reloads wait for the prefetches); a branch for each block's
 // reference 80; without 74; 67 with this part first (see below).
 template <int HD>
@@ -977,9 +976,12 @@ static int pa_plan(const sjd_pages *p, int rows, int n_seqs, int n_groups, int n
     const bool many = p->dtype == 1 && p->head_dim <= 128 && most >= 64 && (entries >> 7) * p->n_kv_heads >= 256;
     const bool two = row <= 512 && ((n_groups && most > 16) || (entries >> 5) * p->n_kv_heads >= 384);
     pl->rows_shift = many ? 7 : two ? 5 : 4;
-    // Splits where tiles are few, as many as workgroups are resident, which registers decide (one query of 32 heads, 4 k positions, fp32: 32.7 with 512 splits, 35.4 with 384; 16
-    // queries behind a prefix, tiles of 32 rows, bf16: 27.0 with 384, 31.5 with 512).  Windows of many rows lose by being cut: 8 x 16 queries of 32 heads, 1.2 k positions, fp32
-    // 52 whole, 62 .. 68 cut.  Every segment has a last tile that is not full.
+    // Splits where tiles are few, about as many as workgroups are resident (one query of 32 heads, 4 k positions, fp32: 32.7 with 512 splits, 35.4 with 384).  Whole tiles take part of
+    // that room: 16 queries behind a prefix, tiles of 32 rows of heads of 128, bf16, of which 512 are resident too: 27.0 with 384, 31.5 with 512.  Windows of many rows lose by being cut:
+    // 8 x 16 queries of 32 heads, 1.2 k positions, fp32 52 whole, 62 .. 68 cut.  Every segment has a last tile that is not full.  The bounds on tiles (320, 512) and the 8 blocks
+    // of the shortest split stand on these alone.
+    // Tables of up to 1024 positions are never cut, whatever the lengths: one sequence of 1 or 16 rows, 32 heads of 128, whole / cut: bf16 100 positions 6.1 / 7.9, 272 8.1 / 9.8, 688
+    // 11.0 / 10.1, 1000 14.5 / 11.1; fp32 9.2 / 11.1, 14.5 / 14.3, 24.0 / 16.4, 29.6 / 17.6.  So whole walks of more than about 500 (bf16) or 300 positions lose.
     const int64_t own = (entries >> pl->rows_shift) + n_seqs, shared = n_groups ? (entries >> pl->rows_shift) + n_groups : 0;
     const int64_t nblk = ((int64_t)width * p->page + 31) / 32;
     const bool few = own * p->n_kv_heads < (mean > 64 ? 320 : 512);
