@@ -254,3 +254,82 @@ def test_a_pool_of_no_dimensions_is_refused(B):
             with pytest.raises(B.SjdError) as e:
                 f()
             assert e.value.code == B.SJD_EINVAL
+
+
+# ---- calls that the header allows ----------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("length,tokens,heads,kv,width,more", SHAPES)
+def test_what_masks_hide_of_the_keys(B, length, tokens, heads, kv, width, more, dtype):
+    """NaN and infinities in keys behind the last token, to the bit; in a key of the last token of a sequence: that row alone"""
+    c = filled(B, length, tokens, kv, width, more, 64, dtype, lambda p, k: k)
+    q = rnd(4, sum(tokens), heads, 64).double().numpy()
+    clean, _ = attended(c, q, length, tokens, heads, 0.125, more)
+    at, _ = R.record_at(64, c.bf16)
+    at = torch.from_numpy(at).cuda()
+    for b, n in enumerate(length):
+        end = n + tokens[b]
+        for p in range(end, (end + 31) // 32 * 32):
+            c.cache[c.table[b, p // 32]][:, 0, at[p % 32]] = float("nan") if p % 2 else float("inf")
+    got, _ = attended(c, q, length, tokens, heads, 0.125, more)
+    assert np.array_equal(got, clean)
+    row = 0
+    for b, n in enumerate(length):
+        row += tokens[b]
+        p = n + tokens[b] - 1
+        c.cache[c.table[b, p // 32]][:, 0, at[p % 32, 5]] = float("nan")
+        clean[row - 1] = np.nan
+    got, _ = attended(c, q, length, tokens, heads, 0.125, more)
+    assert np.array_equal(got, clean, equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("length,tokens,heads,kv,width,more", SHAPES)
+def test_a_query_that_is_not_finite_stays_alone(B, length, tokens, heads, kv, width, more, dtype):
+    c = filled(B, length, tokens, kv, width, more, 64, dtype, lambda p, k: k)
+    q = rnd(4, sum(tokens), heads, 64).double().numpy()
+    clean, _ = attended(c, q, length, tokens, heads, 0.125, more)
+    q[1, 1, 3], q[len(q) - 1, heads - 1, 60] = np.nan, np.nan
+    got, _ = attended(c, q, length, tokens, heads, 0.125, more)
+    clean[1, 1] = clean[len(q) - 1, heads - 1] = np.nan
+    assert np.array_equal(got, clean, equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("length,tokens,heads,kv,width,more", SHAPES)
+def test_rows_before_the_first_sequence(B, length, tokens, heads, kv, width, more, dtype):
+    """starts from 5 on give the same bits five rows further on, and leave the rows before them"""
+    c = filled(B, length, tokens, kv, width, more, 64, dtype, lambda p, k: k)
+    rows, start = sum(tokens), np.concatenate(([0], np.cumsum(tokens)))
+    x = rnd(4, rows + 5, (heads + 2 * kv) * 64).to(c.cache.dtype).cuda()
+    q, k, v = x[:, :heads * 64], x[:, heads * 64:(heads + kv) * 64], x[:, (heads + kv) * 64:]
+    turns = torch.from_numpy(B.sjd_rope_turns(10000.0, 64)).cuda()
+    ws = torch.full((B.sjd_page_attention_workspace(c.pages, rows + 5, len(length), len(more.get("prefix", [])), heads, width),), 0xFF, dtype=torch.uint8, device="cuda")
+    results = []
+    for shift in (5, 0):
+        cache, part = c.cache.clone(), slice(5 - shift, None)
+        turned, out = (torch.full((rows + shift, heads * 64), 7.0, dtype=x.dtype, device="cuda") for _ in range(2))
+        s, n, table = ints((start + shift).tolist()), ints(length), c.dev()
+        B.sjd_page_append(c.pages, k[part], v[part], s, n, table, cache, turns=turns, q=q[part], q_out=turned)
+        B.sjd_page_attention(c.pages, turned, s, n, table, cache, out, ws, 0.125, **{key: ints(y) for key, y in more.items()})
+        assert (turned[:shift] == 7).all() and (out[:shift] == 7).all()
+        results.append((cache, turned[shift:], out[shift:]))
+    # (five rows more can choose other tiles: each result is off by at most 2^-8 + 2^-8 (bf16), 2^-12 (fp32: scores up to 15 off by 72 roundings, 470 of sums) of the largest value)
+    assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
+    assert (results[0][2].double() - results[1][2].double()).abs().max() <= (2.0 ** -6 if c.bf16 else 2.0 ** -11) * c.cache.double().abs().max()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("page,length,tokens", [(1024, [1000, 2040], [40, 9]), (65536, [1030, 0], [3, 33]), (65536, [65530, 65536 + 31], [9, 2])])
+def test_long_pages(B, page, length, tokens, dtype):
+    c = Paged(B, 2, 2, 32, page, 3 if page == 1024 else 2, dtype, spare=1)
+    c.append(length, tokens, heads=2, t=B.sjd_rope_turns(10000.0, 32))
+    c.check(length, tokens, 4)
+    c.check(length, tokens, 4, window=700, sinks=5)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("heads,kv,tokens", [(4096, 1, [2, 1]), (4096, 4096, [1, 2]), (4095, 4095, [1, 0]), (999, 333, [3, 1])])
+def test_as_many_heads_as_there_may_be(B, heads, kv, tokens, dtype):
+    c = Paged(B, 2, kv, 32, 32, 2, dtype)
+    c.append([30, 5], tokens, heads=heads, t=B.sjd_rope_turns(10000.0, 32))
+    c.check([30, 5], tokens, heads)
